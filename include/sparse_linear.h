@@ -187,6 +187,170 @@ sl_status quantize_act(const float *x_dev, int64_t numel, float scale, int8_t *q
 sl_status quantize_act_layout(const float *x_dev, int64_t rows, int32_t cols, float scale, int8_t *q_dev,
                               int32_t q_layout, void *hip_stream);
 
+/*
+ * What lies between the linears of an encoder layer: the attention core
+ * between the QKV and the attention-output linears, and the residual sum with
+ * its norms between a linear's output and the next linear's input (Appendix
+ * "Graph optimization": LayerNorm among the post-operators of a linear).
+ * Serving only, like the linears. The calls allocate nothing, never
+ * synchronise and run on hip_stream; arguments come in a struct that is read
+ * before the call returns. Sums, softmax statistics and norms are held in fp32.
+ */
+typedef enum {
+    SL_NORM_NONE = 0,
+    SL_NORM_LAYER = 1, /* (x - mean) / sqrt(var + eps) * gamma + beta, var over all cols */
+    SL_NORM_RMS = 2    /* x / sqrt(mean(x^2) + eps) * gamma + beta                       */
+} sl_norm_kind;
+
+typedef enum {
+    SL_ACT_NONE = 0,
+    SL_ACT_F32 = 1, /* fp32, row-major                                        */
+    SL_ACT_I8 = 2   /* int8 codes of a per-tensor scale, in either sl_layout  */
+} sl_act_type;
+
+typedef enum {
+    SL_GATE_NONE = 0,
+    SL_GATE_CHANNEL = 1, /* [cols]        */
+    SL_GATE_TOKEN = 2,   /* [rows]        */
+    SL_GATE_ELEMENT = 3  /* [rows x cols] */
+} sl_gate_kind;
+
+/*
+ * One boundary between two blocks of a layer, for every row:
+ *   t = post(y)                          (post: norm of the block's output)
+ *   h = residual_scale * r + gate * t
+ *   u = norm(h)                          (norm before the next block)
+ *   q = clamp(rint(u * (1 / out_scale)), -127, 127)
+ * Pointers are device memory; fp32 ones 4-byte, block-layout ones 16-byte aligned.
+ *   rows            >= 0 (0: no-op)
+ *   cols            1 .. 65535
+ *   y, y_type       SL_ACT_F32 or SL_ACT_I8 (y_layout, y_scale finite and > 0)
+ *   r, r_type       SL_ACT_NONE, SL_ACT_F32 or SL_ACT_I8 (r_layout, r_scale)
+ *   residual_scale  finite
+ *   gate            fp32 of gate_kind's shape, NULL for SL_GATE_NONE
+ *   post_kind, norm_kind  sl_norm_kind; SL_NORM_NONE hands its input on
+ *   gamma, beta     [cols] fp32 of each norm; NULL: 1 and 0
+ *   eps             finite, >= 0 (both norms)
+ *   h, u            [rows x cols] fp32 outputs, q int8 in q_layout (out_scale
+ *                   finite and > 0); NULL: not written, one at least is given.
+ *                   h or u may be y or r themselves (fp32); otherwise outputs
+ *                   overlap no input.
+ * Padding bytes of a block-layout q are unspecified.
+ * Errors: SL_ERR_INVALID_ARG, SL_ERR_SHAPE (rows, cols).
+ */
+typedef struct {
+    int64_t rows;
+    const void *y;
+    const void *r;
+    const float *gate;
+    const float *post_gamma;
+    const float *post_beta;
+    const float *gamma;
+    const float *beta;
+    float *h;
+    float *u;
+    int8_t *q;
+    int32_t cols;
+    int32_t y_type;
+    int32_t y_layout;
+    int32_t r_type;
+    int32_t r_layout;
+    int32_t gate_kind;
+    int32_t post_kind;
+    int32_t norm_kind;
+    int32_t q_layout;
+    float y_scale;
+    float r_scale;
+    float residual_scale;
+    float eps;
+    float out_scale;
+} sl_residual_norm_args;
+
+sl_status residual_norm(const sl_residual_norm_args *args, void *hip_stream);
+
+/* Keys of a selectable block of attention_run and attention_select. */
+#define SL_KEY_BLOCK 64
+
+/*
+ * The attention core of an encoder, on the int8 output of a fused QKV linear.
+ * A batch's sequences lie one after the other in the token dimension: sequence
+ * s is tokens seq_start[s] .. seq_start[s+1]-1. For every sequence, its query
+ * i, its head a and key/value head a / (n_heads / n_kv_heads), with the exact
+ * integers q.k:
+ *   z_j = x_scale^2 * softmax_scale * (q_i . k_j),  j < key_len[s]
+ *   y_i = x_scale * sum_j softmax(z)_j v_j
+ * (no key: y_i = 0). With `blocks` only the listed blocks of 64 consecutive
+ * keys of the sequence take part: blocks[s][a][i / query_block][0 .. top_k-1]
+ * as attention_select writes them (numbers outside the sequence's blocks,
+ * such as -1, are skipped; a number listed twice counts twice).
+ *   x           [m_tokens x (n_heads + 2 n_kv_heads) * head_dim] int8 codes in
+ *               x_layout: all query heads, then all key heads, then all value
+ *               heads; 16-byte aligned
+ *   m_tokens    0 .. 2^31 - 256 (0: no-op)
+ *   n_heads     a multiple of n_kv_heads, both >= 1
+ *   head_dim    a multiple of 16, 16 .. 128
+ *   seq_start   [n_seq + 1] int32 device, ascending, within 0 .. m_tokens
+ *               (values outside are brought into that range). Tokens of no
+ *               sequence are not written.
+ *   key_len     [n_seq] int32 device, valid keys of each sequence (brought
+ *               into 0 .. its length), or NULL for all. Queries past it are
+ *               computed like the others.
+ *   max_len     length of the longest sequence, 0 (no-op) .. 2^31 - 256: what the launch is sized by
+ *               (longer sequences are still computed whole without `blocks`; with
+ *               it, queries from ceil(max_len / query_block) blocks on have no list
+ *               and give 0)
+ *   query_block 16, 32, 64 or 128; top_k >= 1 (read only with `blocks`)
+ *   kind        SL_EPI_F32 (y fp32, row-major) or SL_EPI_I8 (codes of out_scale
+ *               in y_layout)
+ *   y           [m_tokens x n_heads * head_dim], 16-byte aligned
+ * In fp32 results softmax weights enter the products with 22 bits, in int8
+ * ones with 11.
+ * Errors: SL_ERR_INVALID_ARG, SL_ERR_SHAPE (sizes), SL_ERR_UNSUPPORTED (more
+ * work items than a launch takes).
+ */
+typedef struct {
+    const int8_t *x;
+    int64_t m_tokens;
+    const int32_t *seq_start;
+    const int32_t *key_len;
+    const int32_t *blocks;
+    void *y;
+    int32_t n_seq;
+    int32_t max_len;
+    int32_t x_layout;
+    int32_t n_heads;
+    int32_t n_kv_heads;
+    int32_t head_dim;
+    int32_t top_k;
+    int32_t query_block;
+    int32_t kind;
+    int32_t y_layout;
+    float x_scale;
+    float softmax_scale;
+    float out_scale;
+} sl_attention_args;
+
+sl_status attention_run(const sl_attention_args *args, void *hip_stream);
+
+/*
+ * The key blocks that each block of query_block queries attends to, by a cheap
+ * score: with Q the sum of the query block's codes and K_b the sum of key
+ * block b's codes (of a last block of n < 64 keys: rint(64 * sum / n)),
+ *   score_b = Q . K_b            (exact whole numbers)
+ * and the top_k blocks of largest score, ties to the lowest number.
+ *   blocks     [n_seq][n_heads][ceil(max_len / query_block)][top_k] int32:
+ *              ascending, then -1; all -1 where a sequence has no such query
+ *              block or no key.
+ *   workspace  attention_select_workspace(args) bytes, 16-byte aligned, held
+ *              until the stream has passed the call
+ * args: as for attention_run (blocks, y, kind, y_layout and the scales are not
+ * read); max_len at most 262144 (SL_ERR_UNSUPPORTED), and no sequence longer
+ * than max_len (its blocks from there on are not considered).
+ */
+int64_t attention_select_workspace(const sl_attention_args *args);
+sl_status attention_select(const sl_attention_args *args, int32_t *blocks, void *workspace, int64_t workspace_bytes,
+                           void *hip_stream);
+
 /* Rebuild the dense [n_out x k_in] int8 weight from the handle's GPU tile
  * image (host mirror), into caller memory w_host. Round trip of the packer. */
 sl_status sparse_linear_unpack(const sl_packed_weight *w, int8_t *w_host);

@@ -17,11 +17,20 @@ matrix cores read them in:
     h = pw1.run(q, x_scale, sl.EPI_I8_GELU, out_scale=so, m_tokens=M,
                 x_layout=sl.LAYOUT_T16X32, y_layout=sl.LAYOUT_T16X32)
     y = pw2.run(h, so, sl.EPI_F32, m_tokens=M, x_layout=sl.LAYOUT_T16X32)   # fp32 [M, N2]
+
+Between the linears of an encoder layer (a batch's sequences one after the other
+in the token dimension, seq_start their first tokens and the end):
+
+    a = sl.attention(qkv, s_qkv, seq_start, max_len, n_heads, head_dim, out_scale=s_a)      # int8 -> int8
+    blocks = sl.select_blocks(qkv, seq_start, max_len, n_heads, head_dim, top_k)            # long sequences:
+    a = sl.attention(qkv, s_qkv, seq_start, max_len, n_heads, head_dim, out_scale=s_a, blocks=blocks)
+    _, u, q = sl.residual_norm(y, gamma, beta, residual=x, keep_norm=True, out_scale=s_q)   # LayerNorm(x + y)
 """
 from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional
 
 import numpy as np
@@ -32,6 +41,10 @@ LIB_PATH = os.path.join(HERE, "libsparse_linear.so")
 EPI_ACC_I32, EPI_F32, EPI_F32_GELU, EPI_I8, EPI_I8_GELU = 0, 1, 2, 3, 4
 EPI_BY_NAME = {"acc_i32": 0, "f32": 1, "f32_gelu": 2, "i8": 3, "i8_gelu": 4}
 LAYOUT_ROWS, LAYOUT_T16X32 = 0, 1
+NORM_NONE, NORM_LAYER, NORM_RMS = 0, 1, 2
+GATE_NONE, GATE_CHANNEL, GATE_TOKEN, GATE_ELEMENT = 0, 1, 2, 3
+ACT_NONE, ACT_F32, ACT_I8 = 0, 1, 2
+KEY_BLOCK = 64  # keys of a selectable block
 
 SL_OK = 0
 STATUS = {0: "SL_OK", -1: "SL_ERR_INVALID_ARG", -2: "SL_ERR_SHAPE", -3: "SL_ERR_HIP", -4: "SL_ERR_OOM",
@@ -39,7 +52,8 @@ STATUS = {0: "SL_OK", -1: "SL_ERR_INVALID_ARG", -2: "SL_ERR_SHAPE", -3: "SL_ERR_
 
 # every symbol include/sparse_linear.h declares
 EXPORTS = ("sparse_linear_pack", "sparse_linear_pack_host", "sparse_linear_run", "sparse_linear_run_layout",
-           "quantize_act", "quantize_act_layout",
+           "quantize_act", "quantize_act_layout", "residual_norm", "attention_run", "attention_select",
+           "attention_select_workspace",
            "sparse_linear_unpack", "sparse_linear_info", "sparse_linear_export_bsr",
            "sparse_linear_tile_stats", "sparse_linear_free", "sl_status_string", "sl_last_error",
            "sl_abi_version", "sl_last_path", "sl_reload_env", "sl_gelu_table_codes")
@@ -74,12 +88,17 @@ def load() -> ctypes.CDLL:
     lib.sparse_linear_run_layout.argtypes = [vp, vp, i32, i64, f32, i32, f32, vp, i32, vp]
     lib.quantize_act.argtypes = [vp, i64, f32, vp, vp]
     lib.quantize_act_layout.argtypes = [vp, i64, i32, f32, vp, i32, vp]
+    lib.residual_norm.argtypes = [vp, vp]
+    lib.attention_run.argtypes = [vp, vp]
+    lib.attention_select.argtypes = [vp, vp, vp, i64, vp]
+    lib.attention_select_workspace.argtypes = [vp]
+    lib.attention_select_workspace.restype = i64
     lib.sparse_linear_unpack.argtypes = [vp, vp]
     lib.sparse_linear_info.argtypes = [vp, vp, vp, vp]
     lib.sparse_linear_export_bsr.argtypes = [vp, vp, vp, vp]
     lib.sparse_linear_tile_stats.argtypes = [vp, vp, vp, vp, vp]
     for name in ("sparse_linear_pack", "sparse_linear_pack_host", "sparse_linear_run", "sparse_linear_run_layout",
-                 "quantize_act", "quantize_act_layout",
+                 "quantize_act", "quantize_act_layout", "residual_norm", "attention_run", "attention_select",
                  "sparse_linear_unpack", "sparse_linear_info", "sparse_linear_export_bsr",
                  "sparse_linear_tile_stats"):
         getattr(lib, name).restype = i32
@@ -336,4 +355,188 @@ def quantize_act(x, scale: float, out=None, stream=None, layout: int = LAYOUT_RO
     _check(load().quantize_act_layout(x.data_ptr(), rows, cols, float(scale), out.data_ptr(), int(layout),
                                       _stream_ptr(stream)),
            "quantize_act_layout")
+    return out
+
+
+# --- between the linears ------------------------------------------------------
+
+# sl_residual_norm_args and sl_attention_args, field by field
+_NORM_ARGS = struct.Struct("q10P9i5f0q")
+_ATTN_ARGS = struct.Struct("Pq4P10i3f0q")
+
+
+def _act_type(x, name: str, layout: int, shape) -> int:
+    """ACT_F32 or ACT_I8 of a CUDA activation tensor that holds [rows, cols] = shape."""
+    torch = _torch
+    if not x.is_cuda or not x.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous CUDA tensor")
+    if x.dtype == torch.float32:
+        if tuple(x.shape) != shape:
+            raise ValueError(f"{name} must be {shape}")
+        return ACT_F32
+    if x.dtype != torch.int8:
+        raise ValueError(f"{name} must be float32 or int8")
+    want = t16x32_shape(*shape) if layout == LAYOUT_T16X32 else shape
+    if tuple(x.shape) != want:
+        raise ValueError(f"{name} must have shape {want}")
+    return ACT_I8
+
+
+def _f32_ptr(x, name: str, *shapes) -> int:
+    """Address of an optional contiguous fp32 CUDA tensor of one of the shapes; 0 for None."""
+    if x is None:
+        return 0
+    if x.dtype != _torch.float32 or not x.is_cuda or not x.is_contiguous() or tuple(x.shape) not in shapes:
+        raise ValueError(f"{name} must be a contiguous CUDA float32 tensor of shape {' or '.join(map(str, shapes))}")
+    return x.data_ptr()
+
+
+def residual_norm(y, gamma=None, beta=None, *, norm: int = NORM_LAYER, eps: float = 1e-12, y_scale: float = 1.0,
+                  residual=None, residual_scale: float = 1.0, r_scale: float = 1.0, gate=None,
+                  post_norm: int = NORM_NONE, post_gamma=None, post_beta=None, keep_sum=False, keep_norm=False,
+                  out_scale: Optional[float] = None, y_layout: int = LAYOUT_ROWS, r_layout: int = LAYOUT_ROWS,
+                  q_layout: int = LAYOUT_ROWS, shape=None, q_out=None, stream=None):
+    """The boundary between two blocks of a layer, in one pass:
+
+        t = post_norm(y);  h = residual_scale * residual + gate * t;  u = norm(h);  q = codes of u / out_scale
+
+    y, residual: fp32 [rows, cols], or int8 codes (of y_scale, r_scale) in
+    y_layout / r_layout; block-layout tensors need shape=(rows, cols). gate: fp32
+    [cols], [rows, 1] or [rows, cols]. Returns (h, u, q): h where keep_sum, u
+    where keep_norm (True, or a fp32 tensor to write to, which may be y or
+    residual itself), q (int8, q_layout) where out_scale is given; None for the
+    others."""
+    torch = _torch or _torch_once()
+    if shape is None:
+        if y.dim() != 2:
+            raise ValueError("shape=(rows, cols) is needed for a y in the block layout")
+        shape = y.shape
+    shape = rows, cols = int(shape[0]), int(shape[1])
+    y_type = _act_type(y, "y", y_layout, shape)
+    r_type = ACT_NONE if residual is None else _act_type(residual, "residual", r_layout, shape)
+    gate_kind = GATE_NONE
+    if gate is not None:
+        gs = tuple(gate.shape)
+        gate_kind = (GATE_CHANNEL if gs == (cols,) else GATE_ELEMENT if gs == shape and cols > 1 else
+                     GATE_TOKEN if gs == (rows, 1) else -1)
+        if gate_kind < 0:
+            raise ValueError(f"gate must be [{cols}], [{rows}, 1] or [{rows}, {cols}]")
+
+    def kept(keep):
+        return None if keep is False or keep is None else \
+            torch.empty(shape, dtype=torch.float32, device=y.device) if keep is True else keep
+
+    h, u, q = kept(keep_sum), kept(keep_norm), None
+    if out_scale is not None:
+        q_shape = t16x32_shape(rows, cols) if q_layout == LAYOUT_T16X32 else shape
+        q = torch.empty(q_shape, dtype=torch.int8, device=y.device) if q_out is None else q_out
+        if q.dtype != torch.int8 or tuple(q.shape) != q_shape or not q.is_contiguous() or not q.is_cuda:
+            raise ValueError(f"q_out must be a contiguous CUDA int8 tensor of shape {q_shape}")
+    args = _NORM_ARGS.pack(
+        rows, y.data_ptr(), 0 if residual is None else residual.data_ptr(),
+        0 if gate is None else _f32_ptr(gate, "gate", tuple(gate.shape)), _f32_ptr(post_gamma, "post_gamma", (cols,)),
+        _f32_ptr(post_beta, "post_beta", (cols,)), _f32_ptr(gamma, "gamma", (cols,)), _f32_ptr(beta, "beta", (cols,)),
+        _f32_ptr(h, "keep_sum", shape), _f32_ptr(u, "keep_norm", shape), 0 if q is None else q.data_ptr(),
+        cols, y_type, y_layout, r_type, r_layout, gate_kind, post_norm, norm, q_layout,
+        y_scale, r_scale, residual_scale, eps, 1.0 if out_scale is None else out_scale)
+    st = load().residual_norm(args, _stream_ptr(stream))
+    if st != SL_OK:
+        _check(st, "residual_norm")
+    return h, u, q
+
+
+def _attention_args(x, seq_start, max_len, n_heads, head_dim, n_kv_heads, key_len, x_layout, m_tokens):
+    """Checks of what attention and select_blocks share; returns (m_tokens, n_kv_heads, n_seq)."""
+    torch = _torch or _torch_once()
+    n_kv = n_heads if n_kv_heads is None else n_kv_heads
+    cols = (n_heads + 2 * n_kv) * head_dim
+    if x.dtype != torch.int8 or not x.is_cuda or not x.is_contiguous():
+        raise ValueError("qkv must be a contiguous CUDA int8 tensor")
+    if x_layout == LAYOUT_T16X32:
+        if m_tokens is None:
+            raise ValueError("m_tokens is required with LAYOUT_T16X32 input")
+        if tuple(x.shape) != t16x32_shape(m_tokens, cols):
+            raise ValueError(f"qkv must have shape {t16x32_shape(m_tokens, cols)}")
+    elif x.dim() != 2 or x.shape[1] != cols or (m_tokens is not None and m_tokens != x.shape[0]):
+        raise ValueError(f"qkv must be [{'M' if m_tokens is None else m_tokens}, {cols}]")
+    else:
+        m_tokens = x.shape[0]
+    for t, name in ((seq_start, "seq_start"), (key_len, "key_len")):
+        if t is not None and (t.dtype != torch.int32 or not t.is_cuda or t.dim() != 1 or not t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous 1-D CUDA int32 tensor")
+    n_seq = seq_start.shape[0] - 1
+    if n_seq < 0 or (key_len is not None and key_len.shape[0] != n_seq):
+        raise ValueError("seq_start has n_seq + 1 entries, key_len n_seq")
+    return m_tokens, n_kv, n_seq
+
+
+def attention(qkv, x_scale: float, seq_start, max_len: int, n_heads: int, head_dim: int, *,
+              n_kv_heads: Optional[int] = None, softmax_scale: Optional[float] = None, key_len=None,
+              kind: int = EPI_I8, out_scale: float = 1.0, blocks=None, query_block: int = 64,
+              x_layout: int = LAYOUT_ROWS, y_layout: int = LAYOUT_ROWS, m_tokens: Optional[int] = None, out=None,
+              stream=None):
+    """The attention core on a QKV linear's int8 output: codes of x_scale, [M,
+    (n_heads + 2 n_kv_heads) * head_dim], query heads first, then keys, then values.
+
+    Sequence s is tokens seq_start[s] .. seq_start[s+1]-1 (int32 on the device;
+    max_len: the longest, which sizes the launch); key_len: valid keys of each,
+    default all. softmax_scale: default 1 / sqrt(head_dim). blocks: lists of
+    select_blocks with the same query_block, to attend to those keys only.
+    Returns [M, n_heads * head_dim]: int8 codes of out_scale (EPI_I8, y_layout) or
+    fp32 (EPI_F32). Tokens of no sequence are left as they are."""
+    m, n_kv, n_seq = _attention_args(qkv, seq_start, max_len, n_heads, head_dim, n_kv_heads, key_len, x_layout,
+                                     m_tokens)
+    torch = _torch
+    cols = n_heads * head_dim
+    dt = _KIND_DTYPE.get(kind)
+    shape = t16x32_shape(m, cols) if y_layout == LAYOUT_T16X32 else (m, cols)
+    if out is None:
+        out = torch.empty(shape, dtype=dt, device=qkv.device)
+    elif out.dtype != dt or tuple(out.shape) != shape or not out.is_contiguous() or not out.is_cuda:
+        raise ValueError("out has the wrong dtype/shape or is not contiguous")
+    lists, top_k = 0, 0
+    if blocks is not None:
+        want = (n_seq, n_heads, -(-max_len // query_block))
+        if blocks.dtype != torch.int32 or not blocks.is_cuda or not blocks.is_contiguous() or blocks.dim() != 4 or \
+                tuple(blocks.shape[:3]) != want:
+            raise ValueError(f"blocks must be a contiguous CUDA int32 tensor of shape {want} and a list each")
+        lists, top_k = blocks.data_ptr(), blocks.shape[3]
+    args = _ATTN_ARGS.pack(qkv.data_ptr(), m, seq_start.data_ptr(), 0 if key_len is None else key_len.data_ptr(), lists,
+                           out.data_ptr(), n_seq, max_len, x_layout, n_heads, n_kv, head_dim, top_k, query_block, kind,
+                           y_layout, x_scale, head_dim ** -0.5 if softmax_scale is None else softmax_scale, out_scale)
+    st = load().attention_run(args, _stream_ptr(stream))
+    if st != SL_OK:
+        _check(st, "attention_run")
+    return out
+
+
+def select_blocks(qkv, seq_start, max_len: int, n_heads: int, head_dim: int, top_k: int, *,
+                  n_kv_heads: Optional[int] = None, query_block: int = 64, key_len=None,
+                  x_layout: int = LAYOUT_ROWS, m_tokens: Optional[int] = None, out=None, stream=None):
+    """For every block of query_block queries and head, the top_k blocks of 64 keys
+    by the product of the pooled queries and keys (whole numbers: exact; ties to
+    the lowest block). Other arguments as attention's. Returns int32 [n_seq,
+    n_heads, ceil(max_len / query_block), top_k], ascending, then -1."""
+    m, n_kv, n_seq = _attention_args(qkv, seq_start, max_len, n_heads, head_dim, n_kv_heads, key_len, x_layout,
+                                     m_tokens)
+    torch = _torch
+    if query_block < 1 or top_k < 1:
+        raise ValueError("query_block and top_k must be >= 1")
+    shape = (n_seq, n_heads, -(-max_len // query_block), top_k)
+    if out is None:
+        out = torch.empty(shape, dtype=torch.int32, device=qkv.device)
+    elif out.dtype != torch.int32 or tuple(out.shape) != shape or not out.is_contiguous() or not out.is_cuda:
+        raise ValueError(f"out must be a contiguous CUDA int32 tensor of shape {shape}")
+    args = _ATTN_ARGS.pack(qkv.data_ptr(), m, seq_start.data_ptr(), 0 if key_len is None else key_len.data_ptr(), 0, 0,
+                           n_seq, max_len, x_layout, n_heads, n_kv, head_dim, top_k, query_block, EPI_F32, LAYOUT_ROWS,
+                           1.0, 1.0, 1.0)
+    lib, s = load(), _stream_ptr(stream)
+    size = lib.attention_select_workspace(args)
+    # (freed on the current stream: another stream's work must be told of it)
+    work = torch.empty(size, dtype=torch.uint8, device=qkv.device)
+    st = lib.attention_select(args, out.data_ptr(), work.data_ptr(), size, s)
+    if stream is not None:
+        work.record_stream(stream)
+    if st != SL_OK:
+        _check(st, "attention_select")
     return out

@@ -23,8 +23,9 @@ BUILD_DIR = os.path.join(ROOT, "_build")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 DEVICE_FLAGS = ["-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
-HOST_SOURCES = ["api.cpp", "pack.cpp", "gelu_table.cpp"]
-HIP_SOURCES = ["kernels.hip", "kernels_direct.hip", "kernels_panel.hip", "kernels_split.hip", "kernels_tile.hip"]
+HOST_SOURCES = ["api.cpp", "pack.cpp", "gelu_table.cpp", "encoder_api.cpp"]
+HIP_SOURCES = ["kernels.hip", "kernels_direct.hip", "kernels_panel.hip", "kernels_split.hip", "kernels_tile.hip",
+               "kernels_norm.hip", "kernels_attention.hip"]
 # the benchmark's measurement probes (copy bandwidth, matrix-instruction
 # throughput): a library of their own, not linked into the layer's
 PROBE_SOURCES = ["probe.hip"]
