@@ -288,7 +288,7 @@ sl_status residual_norm(const sl_residual_norm_args *args, void *hip_stream);
  *               heads; 16-byte aligned
  *   m_tokens    0 .. 2^31 - 256 (0: no-op)
  *   n_heads     a multiple of n_kv_heads, both >= 1
- *   head_dim    a multiple of 16, 16 .. 128
+ *   head_dim    a multiple of 16, 16 .. 128; at most 2^24 features a token of x
  *   seq_start   [n_seq + 1] int32 device, ascending, within 0 .. m_tokens
  *               (values outside are brought into that range). Tokens of no
  *               sequence are not written.

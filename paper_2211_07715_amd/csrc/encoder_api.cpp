@@ -76,8 +76,8 @@ static sl_status check_attention(const sl_attention_args &a)
               "n_heads must be a multiple of n_kv_heads, both >= 1");
     REFUSE_IF(a.head_dim < 16 || a.head_dim > 128 || a.head_dim % 16, SL_ERR_SHAPE,
               "head_dim must be a multiple of 16, 16 .. 128");
-    REFUSE_IF(((int64_t)a.n_heads + 2 * (int64_t)a.n_kv_heads) * a.head_dim > 0x3fffffff, SL_ERR_SHAPE,
-              "too many heads");
+    REFUSE_IF(((int64_t)a.n_heads + 2 * (int64_t)a.n_kv_heads) * a.head_dim > 0x1000000, SL_ERR_SHAPE,
+              "(n_heads + 2 n_kv_heads) * head_dim must be at most 2^24");
     REFUSE_IF(a.n_seq < 0 || a.max_len < 0 || a.max_len > 0x7fffff00, SL_ERR_SHAPE,
               "n_seq and max_len must be >= 0 (max_len at most 2^31 - 256)");
     REFUSE_IF(!layout_known(a.x_layout), SL_ERR_INVALID_ARG, "unknown x_layout %d", a.x_layout);

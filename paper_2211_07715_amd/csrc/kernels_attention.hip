@@ -1,26 +1,35 @@
 // attention_run and attention_select (gfx950).
 //
 // Attention. For one head and a tile of queries, over chunks of 64 keys:
-//   S = K Q^T            int8 x int8 -> int32 on v_mfma_i32_16x16x64_i8, exact
-//   P = 2^(c (S - m))    m: running maximum of a query's S
-//   l += sum P, O += V^T P^T   on v_mfma_f32_16x16x32_f16
+//   S = K Q^T            int8 x int8 -> int32 on v_mfma_i32_32x32x32_i8, exact
+//   P = 2^(c (S - m))    m: about the largest of a query's S
+//   l += sum P, O += V^T P^T   on v_mfma_f32_32x32x16_f16
 // and y = x_scale O / l. S is computed transposed (keys are the matrix
-// instruction's rows, queries its columns) so that a lane's scores all belong
+// instruction's rows, queries its columns), so that a lane's scores all belong
 // to one query and lie where the second product takes its right operand from:
-// lane group g of a 16-key tile holds keys 4g .. 4g+3, and a pair of tiles'
-// scores, rounded to 16 bits, are the 8 values a lane gives to a 32-key
-// product. That product may take the keys in any order as long as V's operand
-// has them in the same one, so V is laid out in LDS in that order.
+// lane half h of a 32-key tile holds keys 8 i + 4 h .. 8 i + 4 h + 3, and its 8
+// scores of 16 keys, rounded to 16 bits, are the 8 values a lane gives to a
+// 16-key product. That product may take the keys in any order as long as V's
+// operand has them in the same one, so V is laid out in LDS in that order.
 //
 // The integer scores meet the exponential without a conversion: the
 // accumulators start at the bits of 1.5 * 2^23 as a float, less m, so that the
 // finished sums read as floats are 1.5 * 2^23 + (S - m) exactly
-// (|S - m| < 2^22 for heads of up to 128 features), and one fused multiply-add
+// (|S - m| <= 2^22 for heads of up to 128 features), and one fused multiply-add
 // gives the exponent.
+//
+// What bounds it: the vector instructions (an exponential 8.3 cycles of a SIMD,
+// a conversion, permute or dot product 4.3, a fused multiply-add 2.6), with the
+// matrix instructions beside them. 32 x 32 ones take less of the issue than
+// 16 x 16 ones of the same work. m may lag behind the running maximum by a
+// factor of 2^8, which 16-bit P leaves room for: it moves, and l and O are
+// rescaled, outside the loop over chunks, which is left for that and entered
+// again (a branch inside would make the compiler copy every accumulator).
 #include <hip/hip_runtime.h>
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "encoder.h"
 #include "sl_device.h"
@@ -34,13 +43,18 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
 constexpr int kChunk = SL_KEY_BLOCK;      // keys of a step
 constexpr int32_t kMagic = 0x4B400000;    // bits of 1.5 * 2^23
 constexpr float kMagicF = 12582912.0f;
-// P carries a factor 2^kBias: values down to 2^-21 of the largest stay normal 16-bit floats
-constexpr float kBias = 7.0f;
-// m may lag behind the running maximum by 2^kLag (P <= 2^(kBias + 1 + kLag) < 65504)
-constexpr float kLag = 7.0f;
+// P carries a factor 2^kFactor (small weights keep more of their bits). A lane's 32 weights of a chunk then sum to
+// 2^(kFactor + 5) at most where m is the maximum; while they sum to less than kMostSum, none is over what 16 bits hold.
+constexpr int kFactor = 7;
+constexpr float kMostSum = 60000.0f;
+// m before the first key: below every score, and close enough that S - m keeps within the offset's 2^22
+constexpr int32_t kLowest = -(1 << 21);
 
 struct AttnArgs {
     const int8_t *x;
@@ -48,10 +62,9 @@ struct AttnArgs {
     void *y;
     int64_t m;
     int64_t n_items;
-    int32_t n_seq, tiles, n_heads, n_kv, hd, cols, x_cb, y_cb;
+    int32_t n_seq, tiles, tq, n_heads, n_kv, hd, cols, x_cb, y_cb;
     int32_t top_k, n_qb;
     float c2, k2, inv_so, xs;
-    int32_t lag;
 };
 
 // tokens first .. first + n - 1 of a sequence and its valid keys
@@ -72,10 +85,17 @@ __device__ __forceinline__ int64_t at(int64_t t, int32_t c, int32_t cols, int32_
     return cb ? t16x32_offset(t, c, cb) : t * cols + c;
 }
 
-__device__ __forceinline__ int group_max(int v)
+// Of the two lanes that hold a query's scores.
+__device__ __forceinline__ int pair_max(int v)
 {
-    v = max(v, __shfl_xor(v, 16));
-    return max(v, __shfl_xor(v, 32));
+    const auto a = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return max((int)a[0], (int)a[1]);
+}
+__device__ __forceinline__ float pair_sum(float v)
+{
+    const int b = __float_as_int(v);
+    const auto a = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    return __int_as_float(a[0]) + __int_as_float(a[1]);
 }
 
 // 4 keys x 4 features of int8 (words k0 .. k3, a byte a feature) as 16-bit
@@ -101,219 +121,506 @@ __device__ __forceinline__ void transpose_to_f16(const uint32_t (&k)[4], u32x2 (
     out[3] = {high(ab2), high(cd2)};
 }
 
-// DT: 16-feature tiles of a head (head_dim <= 16 DT); QT: 16-query tiles of a
-// wave; NW: waves of a workgroup.
-template <int DT, int QT, int NW, bool F32, bool LISTS>
-__global__ __launch_bounds__(64 * NW) void attention_kernel(const AttnArgs a)
+// Where a thread's pieces of a chunk lie: bytes from the chunk's first token's
+// row block. Both layouts advance by a constant from chunk to chunk, so a
+// thread's offsets are computed once.
+struct Rows {
+    const int8_t *base;  // of the sequence (block layout: of the 16-token block of its first token)
+    int32_t skip;        // block layout: tokens of that block before it
+    int32_t cols, cb;
+    int64_t chunk;       // bytes from a chunk to the next
+    __device__ __forceinline__ Rows(const int8_t *x, int32_t first, int32_t cols_, int32_t cb_)
+        : cols(cols_), cb(cb_)
+    {
+        skip = cb ? first & 15 : 0;
+        base = cb ? x + (int64_t)(first >> 4) * cb * 512 : x + (int64_t)first * cols;
+        chunk = cb ? (int64_t)(kChunk / 16) * cb * 512 : (int64_t)kChunk * cols;
+    }
+    // row `key` (less than 2 chunks) and feature c
+    __device__ __forceinline__ uint32_t offset(int32_t key, int32_t c) const
+    {
+        const int32_t t = key + skip;
+        return cb ? (uint32_t)((t >> 4) * cb + (c >> 5)) * 512 + (t & 15) * 32 + (c & 31) : (uint32_t)(key * cols + c);
+    }
+};
+
+// Permutations of the 16-byte pieces of a row in LDS. A 16-byte read is served
+// 16 lanes at a time, lanes 0-3, 12-15 and 20-27 of each 32 and then the others.
+// With a lane a row, these spread each such set of rows over all 64 banks (4.4
+// cycles a read, against 8.5 with rows padded by 16 bytes).
+template <int N>
+__device__ __forceinline__ int kswap(int row)  // key rows of 32 N bytes
 {
-    constexpr int D = 16 * DT;
-    constexpr int KK = (D + 63) / 64;          // 64-feature products of a score
-    constexpr int KS = D + 16, VS = 2 * kChunk + 16;  // LDS bytes of a key, and of a feature of V
-    constexpr int TQ = 16 * QT * NW;
-    __shared__ __attribute__((aligned(16))) char ks[kChunk * KS];
-    __shared__ __attribute__((aligned(16))) char vs[D * VS];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, n16 = lane & 15;
-    const int64_t item = xcd_work_index(blockIdx.x, a.n_items);
-    const int32_t tile = (int32_t)(item % a.tiles);
-    const int32_t head = (int32_t)(item / a.tiles % a.n_heads);
-    const int32_t seq = (int32_t)(item / a.tiles / a.n_heads);
+    return N == 2 ? (row >> 2) & 3 : N == 4 ? (row >> 1) & 7 : (row >> 3) & 1;
+}
+__device__ __forceinline__ int vswap(int row) { return (row >> 1) & 7; }  // value rows of 128 bytes
+
+// N: 32-feature tiles of a head (head_dim <= 32 N); NW: waves, of QT tiles of 32
+// queries each, which share the chunk of keys and values in LDS. Two
+// buffers: the next chunk is loaded into registers while one is multiplied, and
+// written to the other buffer (V transposed) before the barrier.
+//
+// SPLIT > 1 (NW is 1 then): a workgroup is SPLIT waves on the same queries, each
+// with every SPLIT-th chunk in a buffer of its own and no barrier until their m,
+// l and O meet in LDS at the end.
+//
+// At most 256 registers (two waves a SIMD), so that the accumulators are
+// ordinary registers, which the exponentials read without a copy.
+template <int N, int QT, int NW, int SPLIT, bool F32, bool LISTS>
+__global__ __launch_bounds__(64 * NW * SPLIT) __attribute__((amdgpu_waves_per_eu(2))) void attention_kernel(const AttnArgs a)
+{
+    constexpr int D = 32 * N;
+    constexpr int VS = 2 * kChunk;             // LDS bytes of a feature of V (of a key: D)
+    constexpr int KB = kChunk * D, BUF = KB + D * VS;
+    constexpr int NT = 64 * NW;
+    constexpr int KN = kChunk * 2 * N, VN = kChunk / 4 * D / 4;  // a chunk's 16-byte pieces of K and 4 x 4 ones of V
+    constexpr int KP = (KN + NT - 1) / NT, VP = (VN + NT - 1) / NT;  // and a thread's
+    // (the widest heads have no registers for the next chunk: it is loaded when it is written)
+    constexpr bool AHEAD = N <= 3;
+    constexpr int NBUF = SPLIT == 1 ? 2 : 1;  // (one wave's reads and writes of LDS keep their order)
+    static_assert(SPLIT == 1 || (NW == 1 && QT == 1), "one wave a part");
+    // (the parts' O: 16 N floats a lane)
+    constexpr int LDS = SPLIT * std::max(NBUF * BUF, SPLIT > 1 ? 64 * 64 * N : 0);
+    __shared__ __attribute__((aligned(16))) char all_lds[LDS];
+    const int tid = threadIdx.x % NT, lane = tid & 63, wave = tid >> 6, half = lane >> 5, n32 = lane & 31;
+    const int part = SPLIT > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0;
+    char *lds = all_lds + part * (NBUF * BUF);
+    const auto sync = [] {
+        if constexpr (SPLIT == 1)
+            __syncthreads();
+        else
+            asm volatile("" ::: "memory");
+    };
+    const uint32_t item = (uint32_t)xcd_work_index(blockIdx.x, a.n_items);
+    const int32_t tile = (int32_t)(item % (uint32_t)a.tiles);
+    const int32_t head = (int32_t)(item / (uint32_t)a.tiles % (uint32_t)a.n_heads);
+    const int32_t seq = (int32_t)(item / (uint32_t)a.tiles / (uint32_t)a.n_heads);
     const Span sp = span_of(a.seq_start, a.key_len, seq, a.m);
+    if ((int64_t)tile * a.tq >= sp.n) return;
     const int32_t kv = head / (a.n_heads / a.n_kv);
     const int32_t kcol = (a.n_heads + kv) * a.hd, vcol = (a.n_heads + a.n_kv + kv) * a.hd;
-    const int32_t n_blocks = (sp.keys + kChunk - 1) / kChunk;
+    const Rows rows(a.x, sp.first, a.cols, a.x_cb);
 
-    for (int32_t qt = tile; (int64_t)qt * TQ < sp.n; qt += a.tiles) {
-        const int32_t q0 = qt * TQ + wave * 16 * QT;
-        i32x4 q[QT][KK];
+    // A thread's pieces: key and feature of K piece i, first key and feature of
+    // V piece i. Features past the head's are read as its first ones (they meet
+    // zeros of Q, or give sums that are not stored), keys past a short chunk's
+    // as its last one (their weights are zero).
+    const auto kpiece = [&](int i, int &key, int &d) {
+        const int p = tid + i * NT;
+        key = p / (2 * N) % kChunk;
+        d = p % (2 * N) * 16;
+    };
+    const auto vpiece = [&](int i, int &key, int &d) {
+        const int p = tid + i * NT;  // (8 lanes: 32 keys of 4 features, whose stores fill 64 bytes of LDS)
+        key = (p % 8 + p / (2 * D) * 8) % (kChunk / 4) * 4;
+        d = p / 8 % (D / 4) * 4;
+    };
+    uint32_t koff[KP], voff[VP][4], kdst[KP], vdst[VP];
+    const auto offsets = [&](int32_t have) {
 #pragma unroll
-        for (int t = 0; t < QT; ++t) {
-#pragma unroll
-            for (int h = 0; h < KK; ++h) {
-                const int32_t qi = q0 + 16 * t + n16, d = 64 * h + 16 * g;
-                q[t][h] = i32x4{0, 0, 0, 0};
-                if (qi < sp.n && d < a.hd)
-                    q[t][h] = *reinterpret_cast<const i32x4 *>(
-                        a.x + at((int64_t)sp.first + qi, head * a.hd + d, a.cols, a.x_cb));
-            }
+        for (int i = 0; i < KP; ++i) {
+            int key, d;
+            kpiece(i, key, d);
+            koff[i] = rows.offset(min(key, have - 1), kcol + (d < a.hd ? d : 0));
         }
-        f32x4 o[QT][DT], l[QT];
-        int32_t m[QT];
 #pragma unroll
-        for (int t = 0; t < QT; ++t) {
-            m[t] = 0;
-            l[t] = f32x4{0, 0, 0, 0};
+        for (int i = 0; i < VP; ++i) {
+            int key, d;
+            vpiece(i, key, d);
 #pragma unroll
-            for (int d = 0; d < DT; ++d) o[t][d] = f32x4{0, 0, 0, 0};
+            for (int j = 0; j < 4; ++j) voff[i][j] = rows.offset(min(key + j, have - 1), vcol + (d < a.hd ? d : 0));
         }
-        const int32_t steps = LISTS ? (qt < a.n_qb ? a.top_k : 0) : n_blocks;
-        const int32_t *list = a.blocks + (((int64_t)seq * a.n_heads + head) * a.n_qb + qt) * a.top_k;
-        bool first = true;
-        for (int32_t step = 0; step < steps; ++step) {
-            const int32_t b = LISTS ? list[step] : step;
-            if (LISTS && (uint32_t)b >= (uint32_t)n_blocks) continue;
-            const int32_t k0 = b * kChunk, have = min(sp.keys - k0, kChunk);
-            __syncthreads();
-            // stage: keys as they are (16-byte pieces), values by 4 keys x 4 features
-            for (int i = tid; i < kChunk * DT; i += 64 * NW) {
-                const int key = i / DT, d = i % DT * 16;
-                i32x4 v = {0, 0, 0, 0};
-                if (key < have && d < a.hd)
-                    v = *reinterpret_cast<const i32x4 *>(
-                        a.x + at((int64_t)sp.first + k0 + key, kcol + d, a.cols, a.x_cb));
-                *reinterpret_cast<i32x4 *>(ks + key * KS + d) = v;
-            }
-            for (int i = tid; i < kChunk / 4 * D / 4; i += 64 * NW) {
-                const int kq = i / (D / 4), d = i % (D / 4) * 4;  // keys 4 kq .. 4 kq + 3
-                uint32_t w[4] = {0, 0, 0, 0};
+    };
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (4 * kq + j < have && d < a.hd)
-                        w[j] = *reinterpret_cast<const uint32_t *>(
-                            a.x + at((int64_t)sp.first + k0 + 4 * kq + j, vcol + d, a.cols, a.x_cb));
-                }
+    for (int i = 0; i < KP; ++i) {
+        int key, d;
+        kpiece(i, key, d);
+        kdst[i] = key * D + 16 * (d / 16 ^ kswap<N>(key));
+    }
+#pragma unroll
+    for (int i = 0; i < VP; ++i) {
+        int key, d;
+        vpiece(i, key, d);
+        // place of keys 4 q .. 4 q + 3 of 16 in a feature's row: their lane half's 8, first or second 4
+        const int q = key / 4, pos = (q >> 2) * 16 + (q & 1) * 8 + ((q >> 1) & 1) * 4;
+        // row of a feature: lane half h of a tile's rows 8 x + 4 h + b then holds features 16 N h + 16 tile + 4 x + b
+        const int row = 32 * (d / 16 % N) + 8 * (d / 4 % 4) + 4 * (d / (16 * N));
+        vdst[i] = KB + row * VS + ((2 * pos) ^ (16 * vswap(row)));
+    }
+    i32x4 kreg[KP];
+    uint32_t vreg[VP][4];
+    const auto load = [&](int32_t b) __attribute__((always_inline)) {
+        // (the offsets are in bounds: the resource only spares the lanes 64-bit addresses)
+        const auto x = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(rows.base + b * rows.chunk), 0, 0x7fffffff,
+                                                         kRsrcWord3);
+#pragma unroll
+        for (int i = 0; i < KP; ++i)
+            kreg[i] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(x, koff[i], 0, 0));
+#pragma unroll
+        for (int i = 0; i < VP; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) vreg[i][j] = __builtin_amdgcn_raw_buffer_load_b32(x, voff[i][j], 0, 0);
+    };
+    const auto stage = [&](char *buf) {
+#pragma unroll
+        for (int i = 0; i < KP; ++i)
+            if (KP * NT == KN || tid + i * NT < KN) *reinterpret_cast<i32x4 *>(buf + kdst[i]) = kreg[i];
+#pragma unroll
+        for (int i = 0; i < VP; ++i) {
+            if (VP * NT == VN || tid + i * NT < VN) {
                 u32x2 out[4];
-                transpose_to_f16(w, out);
-                // place of the 4 keys in a feature's row: their lane group's 8 of the 32, first or second tile
-                const int pos = (kq >> 3) * 32 + (kq & 3) * 8 + ((kq >> 2) & 1) * 4;
-                // row of feature 4 DT x + 4 y + j: 16 y + 4 x + j, so that a lane's sums are consecutive features
-                const int row = 16 * ((d >> 2) % DT) + 4 * (d / (4 * DT));
-#pragma unroll
-                for (int j = 0; j < 4; ++j) *reinterpret_cast<u32x2 *>(vs + (row + j) * VS + 2 * pos) = out[j];
+                transpose_to_f16(vreg[i], out);
+                // (of rows 4 x .. 4 x + 3, the last two have the lowest bit of the swap set)
+                char *to = buf + vdst[i], *to2 = buf + (vdst[i] ^ 16);
+                *reinterpret_cast<u32x2 *>(to) = out[0];
+                *reinterpret_cast<u32x2 *>(to + VS) = out[1];
+                *reinterpret_cast<u32x2 *>(to2 + 2 * VS) = out[2];
+                *reinterpret_cast<u32x2 *>(to2 + 3 * VS) = out[3];
             }
-            __syncthreads();
-#pragma unroll
-            for (int t = 0; t < QT; ++t) {
-                i32x4 s[4];
-#pragma unroll
-                for (int kt = 0; kt < 4; ++kt) {
-                    const int32_t z = kMagic - m[t];
-                    s[kt] = i32x4{z, z, z, z};
-#pragma unroll
-                    for (int h = 0; h < KK; ++h) {
-                        i32x4 k = {0, 0, 0, 0};
-                        if (64 * h + 16 * g < D)
-                            k = *reinterpret_cast<const i32x4 *>(ks + (16 * kt + n16) * KS + 64 * h + 16 * g);
-                        s[kt] = __builtin_amdgcn_mfma_i32_16x16x64_i8(k, q[t][h], s[kt], 0, 0, 0);
-                    }
-                }
-                if (have < kChunk) {
-#pragma unroll
-                    for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (16 * kt + 4 * g + r >= have) s[kt][r] = 0;
-                }
-                int top = s[0][0];
-#pragma unroll
-                for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) top = max(top, s[kt][r]);
-                const int up = group_max(top) - kMagic;
-                if (first || __any(up > a.lag)) {
-                    const int by = first ? up : max(up, 0);
-                    const float f = first ? 1.0f : __builtin_amdgcn_exp2f(-(float)by * a.c2);
-                    m[t] += by;
-                    l[t] *= f;
-#pragma unroll
-                    for (int d = 0; d < DT; ++d) o[t][d] *= f;
-#pragma unroll
-                    for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) s[kt][r] -= by;
-                }
-                f16x8 p[2], p2[2];
-#pragma unroll
-                for (int kt = 0; kt < 4; ++kt) {
-                    float e[4];
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        e[r] = __builtin_amdgcn_exp2f(fmaf(__int_as_float(s[kt][r]), a.c2, a.k2));
-                        if (have < kChunk && 16 * kt + 4 * g + r >= have) e[r] = 0.0f;
-                    }
-#pragma unroll
-                    for (int r = 0; r < 4; r += 2) {
-                        const auto hi = __builtin_amdgcn_cvt_pkrtz(e[r], e[r + 1]);
-                        p[kt / 2][(kt & 1) * 4 + r] = hi[0];
-                        p[kt / 2][(kt & 1) * 4 + r + 1] = hi[1];
-                        if constexpr (F32) {
-                            const auto lo = __builtin_amdgcn_cvt_pkrtz(e[r] - (float)hi[0], e[r + 1] - (float)hi[1]);
-                            p2[kt / 2][(kt & 1) * 4 + r] = lo[0];
-                            p2[kt / 2][(kt & 1) * 4 + r + 1] = lo[1];
-                        }
-                    }
-                }
-                const _Float16 one = (_Float16)1.0f;
-                const f16x8 ones = {one, one, one, one, one, one, one, one};
-#pragma unroll
-                for (int w = 0; w < 2; ++w) {
-                    l[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, p[w], l[t], 0, 0, 0);
-                    if constexpr (F32) l[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, p2[w], l[t], 0, 0, 0);
-#pragma unroll
-                    for (int d = 0; d < DT; ++d) {
-                        const f16x8 v =
-                            *reinterpret_cast<const f16x8 *>(vs + (16 * d + n16) * VS + 64 * w + 16 * g);
-                        o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[w], o[t][d], 0, 0, 0);
-                        if constexpr (F32) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p2[w], o[t][d], 0, 0, 0);
-                    }
-                }
-            }
-            first = false;
         }
-        // lane group g holds features 4 DT g .. 4 DT g + 4 DT - 1 of its query
+    };
+
+    for (int32_t qt = tile; (int64_t)qt * a.tq < sp.n; qt += a.tiles) {
+        // (past the queries of a small query block: none)
+        int32_t qi[QT];
+        i32x4 q[QT][N];
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
-            const int32_t qi = q0 + 16 * t + n16;
-            if (qi >= sp.n) continue;
-            const int64_t tok = (int64_t)sp.first + qi;
-            const float f = first ? 0.0f : a.xs / l[t][0];
+            const int32_t i = (wave * QT + t) * 32 + n32;
+            qi[t] = i < a.tq ? qt * a.tq + i : sp.n;
 #pragma unroll
-            for (int d = 0; d < DT; ++d) {
-                const int32_t c = 4 * DT * g + 4 * d;
-                if (c >= a.hd) continue;
-                const f32x4 v = o[t][d] * f;
-                if constexpr (F32) {
-                    store_nt(reinterpret_cast<float *>(a.y) + tok * (a.n_heads * a.hd) + head * a.hd + c, v);
-                } else {
+            for (int h = 0; h < N; ++h) {
+                const int32_t d = 32 * h + 16 * half;
+                q[t][h] = i32x4{0, 0, 0, 0};
+                if (qi[t] < sp.n && d < a.hd)
+                    q[t][h] = *reinterpret_cast<const i32x4 *>(
+                        a.x + at((int64_t)sp.first + qi[t], head * a.hd + d, a.cols, a.x_cb));
+            }
+        }
+        f32x16 o[QT][N];
+        float l[QT];
+        int32_t z[QT];  // what S starts at: kMagic - m
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            l[t] = 0.0f;
+            z[t] = kMagic - kLowest;
+#pragma unroll
+            for (int d = 0; d < N; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[t][d][i] = 0.0f;
+        }
+
+        const auto key_of = [&](int kt, int i) { return 32 * kt + 8 * (i / 4) + 4 * half + i % 4; };
+        // scores of a chunk
+        const auto scores = [&](int t, const char *buf, const i32x16 &from, i32x16 (&s)[2]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt) {
+                s[kt] = from;
+#pragma unroll
+                for (int h = 0; h < N; ++h) {
+                    const int row = 32 * kt + n32;
+                    const i32x4 k = *reinterpret_cast<const i32x4 *>(buf + row * D + 16 * ((2 * h + half) ^ kswap<N>(n32)));
+                    s[kt] = __builtin_amdgcn_mfma_i32_32x32x32_i8(k, q[t][h], s[kt], 0, 0, 0);
+                }
+            }
+        };
+        const auto from_z = [&](int t) {
+            i32x16 v;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = z[t];
+            asm volatile("" : "+v"(v));  // 16 registers for the loop over chunks, not 32 moves in it
+            return v;
+        };
+        // the largest of a lane's (of a chunk of `have` keys, tail: less than a whole one)
+        const auto largest = [&](auto tail, int32_t have, const i32x16 (&s)[2]) __attribute__((always_inline)) {
+            int32_t top = 0;
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (!decltype(tail)::value || key_of(kt, i) < have) top = max(top, s[kt][i]);
+            return top;
+        };
+        // m up to the running maximum
+        const auto raise = [&](int t, int32_t top) __attribute__((always_inline)) {
+            const int32_t by = max(pair_max(top) - kMagic, 0);
+            const float f = __builtin_amdgcn_exp2f(-(float)by * a.c2);
+            z[t] -= by;
+            l[t] *= f;
+#pragma unroll
+            for (int d = 0; d < N; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[t][d][i] *= f;
+        };
+        // weights of a chunk and their sum
+        f16x8 p[QT][4], p2[QT][F32 ? 4 : 1];
+        const auto weights = [&](auto tail, int t, int32_t have, const i32x16 (&s)[2]) __attribute__((always_inline)) {
+            float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {  // 16 keys
+#pragma unroll
+                for (int j = 0; j < 8; j += 2) {
+                    f32x2 e;
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        const int i = 8 * (w & 1) + j + r;
+                        e[r] = __builtin_amdgcn_exp2f(fmaf(__int_as_float(s[w / 2][i]), a.c2, a.k2));
+                        if (decltype(tail)::value && key_of(w / 2, i) >= have) e[r] = 0.0f;
+                    }
+                    const f16x2 ones = {(_Float16)1.0f, (_Float16)1.0f};
+                    const f16x2 hi = __builtin_convertvector(e, f16x2);
+                    sum[w & 1] = __builtin_amdgcn_fdot2(hi, ones, sum[w & 1], false);
+                    p[t][w][j] = hi[0];
+                    p[t][w][j + 1] = hi[1];
+                    if constexpr (F32) {
+                        const f32x2 less = {e[0] - (float)hi[0], e[1] - (float)hi[1]};
+                        const f16x2 lo = __builtin_convertvector(less, f16x2);
+                        sum[w & 1] = __builtin_amdgcn_fdot2(lo, ones, sum[w & 1], false);
+                        p2[t][w][j] = lo[0];
+                        p2[t][w][j + 1] = lo[1];
+                    }
+                }
+            }
+            return sum[0] + sum[1];
+        };
+        const auto multiply = [&](const char *buf) __attribute__((always_inline)) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w)
+#pragma unroll
+                for (int d = 0; d < N; ++d) {
+                    const f16x8 v = *reinterpret_cast<const f16x8 *>(
+                        buf + KB + (32 * d + n32) * VS + 16 * ((2 * w + half) ^ vswap(n32)));
+#pragma unroll
+                    for (int t = 0; t < QT; ++t) {
+                        o[t][d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[t][w], o[t][d], 0, 0, 0);
+                        if constexpr (F32) o[t][d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p2[t][w], o[t][d], 0, 0, 0);
+                    }
+                }
+        };
+
+        // Whole chunks first, then the sequence's short last one. With lists:
+        // 64 numbers at a time, one a lane; those of whole chunks as a mask.
+        const int32_t whole = sp.keys / kChunk, rest = sp.keys % kChunk;
+        const int32_t steps = LISTS ? (qt < a.n_qb ? a.top_k : 0) : whole;
+        const int32_t *list = a.blocks + (((int64_t)seq * a.n_heads + head) * a.n_qb + qt) * a.top_k;
+        int32_t at_step = LISTS ? 0 : part, mine = -1, tails = !LISTS && rest && (SPLIT == 1 || whole % SPLIT == part);
+        uint64_t left = 0;
+        const uint64_t ours = SPLIT == 1 ? ~0ull : 0x1111111111111111ull << part;
+        static_assert(SPLIT == 1 || SPLIT == 4, "every 4th of a list's numbers");
+        const auto next = [&]() -> int32_t {  // the next whole chunk, or -1
+            if constexpr (!LISTS) {
+                const int32_t i = at_step;
+                at_step += SPLIT;
+                return i < steps ? i : -1;
+            } else {
+                while (!left) {
+                    if (at_step >= steps) return -1;
+                    mine = at_step + lane < steps ? list[at_step + lane] : -1;
+                    left = __ballot((uint32_t)mine < (uint32_t)whole) & ours;
+                    if (rest) tails += __popcll(__ballot(mine == whole) & ours);
+                    at_step += 64;
+                }
+                const int i = __builtin_ctzll(left);
+                left &= left - 1;
+                return __builtin_amdgcn_readlane(mine, i);
+            }
+        };
+        offsets(kChunk);
+        i32x16 sc[2];
+        int32_t b = next();
+        if (b >= 0) {
+            load(b);
+            stage(lds);
+            b = next();
+            sync();
+            int32_t buf = 0;
+            if (wave * 32 * QT >= a.tq) {  // a wave without queries only brings chunks in
+                while (b >= 0) {
+                    load(b);
+                    buf ^= BUF;
+                    stage(lds + buf);
+                    b = next();
+                    sync();
+                }
+                goto done;
+            }
+            for (;;) {
+                i32x16 from[QT];
+#pragma unroll
+                for (int t = 0; t < QT; ++t) {
+                    scores(t, lds + buf, from_z(t), sc);
+                    raise(t, largest(std::false_type{}, kChunk, sc));
+                    from[t] = from_z(t);
+                }
+                for (;;) {
+                    if (AHEAD && b >= 0) load(b);  // (again after m has moved)
+                    float sum[QT];
+                    bool over = false;  // (a weight over 65504 makes the sum infinite or, with its remainder, no number)
+#pragma unroll
+                    for (int t = 0; t < QT; ++t) {
+                        scores(t, lds + buf, from[t], sc);
+                        sum[t] = weights(std::false_type{}, t, kChunk, sc);
+                        over |= !(sum[t] < kMostSum);
+                    }
+                    if (__any(over)) break;
+#pragma unroll
+                    for (int t = 0; t < QT; ++t) l[t] += sum[t];
+                    multiply(lds + buf);
+                    if (b < 0) goto done;
+                    if constexpr (NBUF > 1) buf ^= BUF;
+                    if constexpr (!AHEAD) load(b);
+                    stage(lds + buf);
+                    b = next();
+                    sync();
+                }
+            }
+        done:
+            sync();
+        }
+        if (tails > 0) {
+            offsets(rest);
+            load(whole);
+            stage(lds);
+            sync();
+            for (int32_t i = 0; i < tails; ++i) {
+#pragma unroll
+                for (int t = 0; t < QT; ++t) {
+                    scores(t, lds, from_z(t), sc);
+                    raise(t, largest(std::true_type{}, rest, sc));
+                    scores(t, lds, from_z(t), sc);
+                    l[t] += weights(std::true_type{}, t, rest, sc);
+                }
+                multiply(lds);
+            }
+            sync();
+        }
+        if constexpr (SPLIT > 1) {
+            // every part's l and O from the largest m; part w then sums registers 4 N w .. 4 N w + 4 N - 1 of all
+            __shared__ int32_t zs[SPLIT][32];
+            __shared__ float ls[SPLIT][32];
+            l[0] = pair_sum(l[0]);
+            __syncthreads();
+            if (half == 0) {
+                zs[part][n32] = z[0];
+                ls[part][n32] = l[0];
+            }
+            __syncthreads();
+            int32_t zmin = zs[0][n32];
+#pragma unroll
+            for (int w = 1; w < SPLIT; ++w) zmin = min(zmin, zs[w][n32]);
+            const float f = __builtin_amdgcn_exp2f(-(float)(z[0] - zmin) * a.c2);
+            float *mine_o = reinterpret_cast<float *>(all_lds) + part * (64 * 16 * N);
+#pragma unroll
+            for (int d = 0; d < N; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) mine_o[(16 * d + i) * 64 + lane] = o[0][d][i] * f;
+            float sum = 0.0f;
+#pragma unroll
+            for (int w = 0; w < SPLIT; ++w)
+                sum += ls[w][n32] * __builtin_amdgcn_exp2f(-(float)(zs[w][n32] - zmin) * a.c2);
+            __syncthreads();
+            const float g = sum > 0.0f ? a.xs / sum : 0.0f;
+            const int64_t tok = (int64_t)sp.first + qi[0];
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int first = 4 * N * part + 4 * i;
+                f32x4 v = {0, 0, 0, 0};
+#pragma unroll
+                for (int w = 0; w < SPLIT; ++w)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        v[j] += reinterpret_cast<const float *>(all_lds)[w * (64 * 16 * N) + (first + j) * 64 + lane];
+                v *= g;
+                const int32_t c = 16 * N * half + first;
+                if (qi[0] >= sp.n || c >= a.hd) continue;
+                if constexpr (F32)
+                    *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(a.y) + tok * (a.n_heads * a.hd) + head * a.hd + c) = v;
+                else
                     *reinterpret_cast<uint32_t *>(reinterpret_cast<int8_t *>(a.y) +
                                                   at(tok, head * a.hd + c, a.n_heads * a.hd, a.y_cb)) =
                         pack_bytes(requant_bits(v[0], a.inv_so), requant_bits(v[1], a.inv_so),
                                    requant_bits(v[2], a.inv_so), requant_bits(v[3], a.inv_so));
+            }
+            __syncthreads();
+            continue;
+        }
+        // a lane half holds features 16 N half .. 16 N half + 16 N - 1 of its query
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            const float sum = pair_sum(l[t]), f = sum > 0.0f ? a.xs / sum : 0.0f;
+            if (qi[t] >= sp.n) continue;
+            const int64_t tok = (int64_t)sp.first + qi[t];
+            if constexpr (F32) {
+                float *y = reinterpret_cast<float *>(a.y) + tok * (a.n_heads * a.hd) + head * a.hd + 16 * N * half;
+#pragma unroll
+                for (int d = 0; d < N; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4)
+                        if (16 * N * half + 16 * d < a.hd)
+                            *reinterpret_cast<f32x4 *>(y + 16 * d + i) =
+                                f32x4{o[t][d][i], o[t][d][i + 1], o[t][d][i + 2], o[t][d][i + 3]} * f;
+            } else {
+#pragma unroll
+                for (int d = 0; d < N; ++d) {
+                    i32x4 w;
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4)
+                        w[i / 4] = (int)pack_bytes(
+                            requant_bits(o[t][d][i] * f, a.inv_so), requant_bits(o[t][d][i + 1] * f, a.inv_so),
+                            requant_bits(o[t][d][i + 2] * f, a.inv_so), requant_bits(o[t][d][i + 3] * f, a.inv_so));
+                    const int32_t c = 16 * N * half + 16 * d;
+                    if (c < a.hd)
+                        *reinterpret_cast<i32x4 *>(reinterpret_cast<int8_t *>(a.y) +
+                                                   at(tok, head * a.hd + c, a.n_heads * a.hd, a.y_cb)) = w;
                 }
             }
         }
     }
 }
 
-template <int DT, int QT, int NW, bool LISTS>
-sl_status launch_kind(AttnArgs &a, int32_t kind, int32_t max_len, hipStream_t s)
+// tq: queries of a workgroup
+template <int N, int QT, int NW, int SPLIT, bool LISTS, bool F32>
+sl_status launch_shape(AttnArgs &a, int32_t tq, int32_t max_len, hipStream_t s)
 {
-    constexpr int TQ = 16 * QT * NW;
-    a.tiles = (max_len + TQ - 1) / TQ;
+    a.tq = tq;
+    a.tiles = (max_len + tq - 1) / tq;
     a.n_items = (int64_t)a.tiles * a.n_heads * a.n_seq;
-    if (a.n_items > 0x7fffffff / (64 * NW)) {
+    if (a.n_items > 0x7fffffff / (64 * NW * SPLIT)) {
         set_error("too many work items for one launch");
         return SL_ERR_UNSUPPORTED;
     }
-    if (kind == SL_EPI_F32)
-        hipLaunchKernelGGL((attention_kernel<DT, QT, NW, true, LISTS>), dim3((uint32_t)a.n_items), dim3(64 * NW), 0, s,
-                           a);
-    else
-        hipLaunchKernelGGL((attention_kernel<DT, QT, NW, false, LISTS>), dim3((uint32_t)a.n_items), dim3(64 * NW), 0,
-                           s, a);
+    hipLaunchKernelGGL((attention_kernel<N, QT, NW, SPLIT, F32, LISTS>), dim3((uint32_t)a.n_items),
+                       dim3(64 * NW * SPLIT), 0, s, a);
     HIP_TRY(hipGetLastError());
     return SL_OK;
 }
 
-template <int DT>
+template <int N, bool F32>
 sl_status launch_head(AttnArgs &a, const sl_attention_args &args, hipStream_t s)
 {
-    if (!args.blocks) return launch_kind<DT, 1, 4, false>(a, args.kind, args.max_len, s);
-    switch (args.query_block) {
-    case 16: return launch_kind<DT, 1, 1, true>(a, args.kind, args.max_len, s);
-    case 32: return launch_kind<DT, 1, 2, true>(a, args.kind, args.max_len, s);
-    case 64: return launch_kind<DT, 1, 4, true>(a, args.kind, args.max_len, s);
-    default: return launch_kind<DT, 2, 4, true>(a, args.kind, args.max_len, s);
+    const int32_t n = args.max_len, qb = args.query_block;
+    if (!args.blocks) {
+        const int64_t heads = (int64_t)args.n_heads * args.n_seq;
+        const int64_t items = heads * ((n + 127) / 128), wide = heads * ((n + 255) / 256);
+        if constexpr (N <= 2) {
+            if constexpr (!F32)
+                if (n >= 1024 && wide >= 512) return launch_shape<N, 2, 4, 1, false, F32>(a, 256, n, s);
+            if (n >= 256 && items <= 96) return launch_shape<N, 1, 1, 4, false, F32>(a, 32, n, s);
+        }
+        return launch_shape<N, 1, 4, 1, false, F32>(a, 128, n, s);
     }
+    if constexpr (N <= 2) {
+        if (qb <= 32) return launch_shape<N, 1, 1, 1, true, F32>(a, qb, n, s);
+        if (qb == 64) return launch_shape<N, 1, 2, 1, true, F32>(a, qb, n, s);
+    }
+    // (one or two waves would hold a wide head's chunk in too many registers)
+    return launch_shape<N, 1, 4, 1, true, F32>(a, qb, n, s);
+}
+
+template <int N>
+sl_status launch_kind(AttnArgs &a, const sl_attention_args &args, hipStream_t s)
+{
+    return args.kind == SL_EPI_F32 ? launch_head<N, true>(a, args, s) : launch_head<N, false>(a, args, s);
 }
 
 // --- choice of key blocks ----------------------------------------------------
@@ -466,14 +773,18 @@ sl_status launch_attention(const sl_attention_args &args, void *stream)
     int e = 0;
     const double frac = frexp(c2, &e);
     a.c2 = (float)ldexp(nearbyint(ldexp(frac, 22)), e - 22);
-    a.k2 = kBias - kMagicF * a.c2;
-    a.lag = (int32_t)std::min<double>(kLag / std::max((double)a.c2, 1e-30), 1 << 23);
+    // (past 2^24 the offset takes no whole number: weights of neighbouring scores differ by a factor of 2.5 there)
+    const bool fits = kMagicF * a.c2 < 16777216.0f;
+    a.k2 = (fits ? (float)kFactor : 0.0f) - kMagicF * a.c2;
     a.xs = args.x_scale;
     a.inv_so = args.kind == SL_EPI_I8 ? 1.0f / args.out_scale : 1.0f;
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    if (a.hd <= 32) return launch_head<2>(a, args, s);
-    if (a.hd <= 64) return launch_head<4>(a, args, s);
-    return launch_head<8>(a, args, s);
+    switch ((a.hd + 31) / 32) {
+    case 1: return launch_kind<1>(a, args, s);
+    case 2: return launch_kind<2>(a, args, s);
+    case 3: return launch_kind<3>(a, args, s);
+    default: return launch_kind<4>(a, args, s);
+    }
 }
 
 sl_status launch_attention_select(const sl_attention_args &args, int32_t *blocks, void *workspace, void *stream)
