@@ -303,8 +303,7 @@ sl_status residual_norm(const sl_residual_norm_args *args, void *hip_stream);
  *   kind        SL_EPI_F32 (y fp32, row-major) or SL_EPI_I8 (codes of out_scale
  *               in y_layout)
  *   y           [m_tokens x n_heads * head_dim], 16-byte aligned
- * In fp32 results softmax weights enter the products with 22 bits, in int8
- * ones with 11.
+ * Softmax weights enter the products with 22 bits.
  * Errors: SL_ERR_INVALID_ARG, SL_ERR_SHAPE (sizes), SL_ERR_UNSUPPORTED (more
  * work items than a launch takes).
  */
