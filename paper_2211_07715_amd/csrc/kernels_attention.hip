@@ -42,6 +42,9 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
+typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
+typedef int16_t i16x4 __attribute__((ext_vector_type(4)));
+typedef int16_t i16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
@@ -654,113 +657,137 @@ struct SelectArgs {
     int32_t n_seq, n_heads, n_kv, hd, cols, x_cb, top_k, qb, n_qb, max_blocks;
 };
 
-// Pooled keys: one thread a key block and 4 features, over the block's keys.
+// Pooled keys: one wave a key block and 64 features of the keys, 4 features a
+// lane, and every 4th key; all 16 loads of a lane are in flight together.
 __global__ __launch_bounds__(256) void pool_keys_kernel(const SelectArgs a)
 {
-    const int32_t seq = blockIdx.z, b = blockIdx.y;
+    const int32_t seq = blockIdx.z, b = blockIdx.y, lane = threadIdx.x & 63;
     const Span sp = span_of(a.seq_start, a.key_len, seq, a.m);
     const int32_t have = min(sp.keys - b * kChunk, kChunk);
-    const int32_t c = (blockIdx.x * 256 + threadIdx.x) * 4;  // of the key columns
-    if (have <= 0 || c >= a.n_kv * a.hd) return;
-    int32_t sum[4] = {0, 0, 0, 0};
-    for (int32_t j = 0; j < have; ++j) {
-        const int32_t w = *reinterpret_cast<const int32_t *>(
-            a.x + at((int64_t)sp.first + b * kChunk + j, a.n_heads * a.hd + c, a.cols, a.x_cb));
+    const int32_t c = (blockIdx.x * 4 + threadIdx.x / 64) * 64 + lane % 16 * 4;  // of the key columns
+    if (have <= 0) return;
+    const bool mine = c < a.n_kv * a.hd;
+    const Rows rows(a.x, sp.first + b * kChunk, a.cols, a.x_cb);
+    uint32_t w[16];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum[i] += (int8_t)(w >> (8 * i));
+    for (int j = 0; j < 16; ++j) {
+        const int32_t key = 4 * j + lane / 16;
+        w[j] = 0;
+        if (mine && key < have)
+            w[j] = *reinterpret_cast<const uint32_t *>(rows.base + rows.offset(key, a.n_heads * a.hd + c));
     }
-    const int64_t slot = sp.first / kChunk + seq + b;
-    int16_t *out = a.pooled + ((int64_t)(c / 8) * a.slots + slot) * 8 + c % 8;
+    int32_t sum[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] = __builtin_amdgcn_sdot4((int)w[j], 1 << (8 * i), sum[i], false);
+    i16x4 out;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
+        sum[i] += __shfl_xor(sum[i], 16);
+        sum[i] += __shfl_xor(sum[i], 32);
         // (64 sum / have is a half-integer or further than 1 / 128 from one, so its fp32 value rounds as it does)
         out[i] = have == kChunk ? (int16_t)sum[i] : (int16_t)__builtin_rintf((float)(sum[i] * kChunk) / (float)have);
     }
+    const int64_t slot = sp.first / kChunk + seq + b;
+    if (mine && lane < 16)
+        *reinterpret_cast<i16x4 *>(a.pooled + ((int64_t)(c / 8) * a.slots + slot) * 8 + c % 8) = out;
 }
 
-// One wave a query block and head: the sum of its queries, a score a key block
-// (VPL a lane), and the top_k of them. A score has up to 36 bits: products are
-// summed 8 at a time in 32 bits (8 * 2^14 * 2^13 < 2^31), then in 64. The
-// top_k-th largest is found bit by bit, by counting.
+// One wave a head and query block: the sum of its queries, the scores of a
+// lane's VPL key blocks, and the top_k largest. A score has up to 36 bits:
+// products are summed 8 at a time in 32 bits (8 * 2^14 * 2^13 < 2^31), then in
+// 64. The top_k-th largest is found bit by bit, by counting. (Bound by the
+// latency of its steps: four query blocks a wave, which read the pooled keys a
+// quarter as often, took 29 us against 17 at 16384 tokens.)
 template <int VPL>
 __global__ __launch_bounds__(64) void select_blocks_kernel(const SelectArgs a)
 {
     __shared__ int32_t qsum[128];
+    __shared__ __attribute__((aligned(16))) int16_t q16[128];
     const int lane = threadIdx.x;
     const int32_t qb = blockIdx.x, head = blockIdx.y, seq = blockIdx.z;
     const Span sp = span_of(a.seq_start, a.key_len, seq, a.m);
     int32_t *list = a.blocks + (((int64_t)seq * a.n_heads + head) * a.n_qb + qb) * a.top_k;
-    const int32_t rows = min(sp.n - qb * a.qb, a.qb);
-    const int32_t nb = rows > 0 ? min((sp.keys + kChunk - 1) / kChunk, a.max_blocks) : 0;
+    const int32_t rows_n = min(sp.n - qb * a.qb, a.qb);
+    const int32_t nb = rows_n > 0 ? min((sp.keys + kChunk - 1) / kChunk, a.max_blocks) : 0;
     const int32_t take = min(nb, a.top_k);
-    for (int32_t i = take + lane; i < a.top_k; i += 64) list[i] = -1;
-    if (nb == 0) return;
-    if (nb <= a.top_k) {
-        for (int32_t i = lane; i < nb; i += 64) list[i] = i;
+    if (nb <= a.top_k) {  // nothing to choose
+        for (int32_t i = lane; i < a.top_k; i += 64) list[i] = i < take ? i : -1;
         return;
     }
-    for (int d = lane * 4; d < 128; d += 256) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) qsum[d + i] = 0;
-    }
+    qsum[lane] = qsum[lane + 64] = 0;
     __syncthreads();
     {
         // 4 features a lane; lanes beyond the head's features take other rows
         const int quads = a.hd / 4, d = lane % quads * 4, r0 = lane / quads, per = 64 / quads;
-        int32_t sum[4] = {0, 0, 0, 0};
         if (r0 < per) {
-            for (int32_t r = r0; r < rows; r += per) {
-                const int32_t w = *reinterpret_cast<const int32_t *>(
-                    a.x + at((int64_t)sp.first + (int64_t)qb * a.qb + r, head * a.hd + d, a.cols, a.x_cb));
+            int32_t sum[4] = {0, 0, 0, 0};
+            const Rows rows(a.x, sp.first + qb * a.qb, a.cols, a.x_cb);
+#pragma unroll 8
+            for (int32_t r = r0; r < rows_n; r += per) {
+                const int32_t w = *reinterpret_cast<const int32_t *>(rows.base + rows.offset(r, head * a.hd + d));
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sum[i] += (int8_t)(w >> (8 * i));
+                for (int j = 0; j < 4; ++j) sum[j] = __builtin_amdgcn_sdot4(w, 1 << (8 * j), sum[j], false);
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) atomicAdd(&qsum[d + i], sum[i]);  // (whole numbers: the order does not matter)
+            for (int j = 0; j < 4; ++j) atomicAdd(&qsum[d + j], sum[j]);  // (whole numbers: the order does not matter)
         }
     }
     __syncthreads();
+    q16[lane] = (int16_t)qsum[lane];
+    q16[lane + 64] = (int16_t)qsum[lane + 64];
+    __syncthreads();
     const int32_t kv = head / (a.n_heads / a.n_kv);
-    const int64_t slot = sp.first / kChunk + seq;
-    const int16_t *pooled = a.pooled + (int64_t)kv * (a.hd / 8) * a.slots * 8;
+    const int16_t *pooled = a.pooled + ((int64_t)kv * (a.hd / 8) * a.slots + sp.first / kChunk + seq) * 8;
     int64_t v[VPL];
+    constexpr int G = std::min(VPL, 4);  // blocks whose loads are in flight together
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) {
-        const int32_t b = i * 64 + lane;
-        v[i] = -1;  // below every score's unsigned form
-        if (b < nb) {
-            int64_t score = (int64_t)1 << 36;
-            for (int d8 = 0; d8 < a.hd / 8; ++d8) {
-                const int16_t *k = pooled + ((int64_t)d8 * a.slots + slot + b) * 8;
+    for (int j0 = 0; j0 < VPL; j0 += G) {
+#pragma unroll
+        for (int j = 0; j < G; ++j)
+            v[j0 + j] = (j0 + j) * 64 + lane < nb ? (int64_t)1 << 36 : -1;  // (-1: no such block)
+#pragma unroll 4
+        for (int d8 = 0; d8 < a.hd / 8; ++d8) {
+            const i16x8 q = *reinterpret_cast<const i16x8 *>(&q16[8 * d8]);
+            i16x8 k[G];
+#pragma unroll
+            for (int j = 0; j < G; ++j) {
+                k[j] = i16x8{0, 0, 0, 0, 0, 0, 0, 0};
+                if ((j0 + j) * 64 + lane < nb)
+                    k[j] = *reinterpret_cast<const i16x8 *>(pooled + (d8 * a.slots + (j0 + j) * 64 + lane) * 8);
+            }
+#pragma unroll
+            for (int j = 0; j < G; ++j) {
                 int32_t s = 0;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) s += qsum[d8 * 8 + j] * (int32_t)k[j];
-                score += s;
+                for (int e = 0; e < 8; e += 2)
+                    s = __builtin_amdgcn_sdot2(i16x2{k[j][e], k[j][e + 1]}, i16x2{q[e], q[e + 1]}, s, false);
+                v[j0 + j] += s;
             }
-            v[i] = score;
         }
     }
-    // the largest t that take values or more reach
+    // the largest t that top_k values or more reach
     int64_t t = 0;
     for (int bit = 36; bit >= 0; --bit) {
         const int64_t want = t | ((int64_t)1 << bit);
         int32_t count = 0;
 #pragma unroll
-        for (int i = 0; i < VPL; ++i) count += __popcll(__ballot(v[i] >= want));
+        for (int j = 0; j < VPL; ++j) count += __popcll(__ballot(v[j] >= want));
         if (count >= take) t = want;
     }
     int32_t over = 0;
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) over += __popcll(__ballot(v[i] > t));
+    for (int j = 0; j < VPL; ++j) over += __popcll(__ballot(v[j] > t));
     int32_t ties = take - over, out = 0;  // of those that equal t, the first `ties`
     const uint64_t below = ((uint64_t)1 << lane) - 1;
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) {
-        const uint64_t eq = __ballot(v[i] == t);
-        const bool chosen = v[i] > t || (v[i] == t && __popcll(eq & below) < ties);
+    for (int j = 0; j < VPL; ++j) {
+        const uint64_t eq = __ballot(v[j] == t);
+        const bool chosen = v[j] > t || (v[j] == t && __popcll(eq & below) < ties);
         ties -= min(ties, (int32_t)__popcll(eq));
         const uint64_t sel = __ballot(chosen);
-        if (chosen) list[out + __popcll(sel & below)] = i * 64 + lane;
+        if (chosen) list[out + __popcll(sel & below)] = j * 64 + lane;
         out += __popcll(sel);
     }
 }
@@ -834,11 +861,12 @@ sl_status launch_attention_select(const sl_attention_args &args, int32_t *blocks
         return SL_ERR_UNSUPPORTED;
     }
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    hipLaunchKernelGGL(pool_keys_kernel, dim3((a.n_kv * a.hd / 4 + 255) / 256, a.max_blocks, a.n_seq), dim3(256), 0, s,
-                       a);
+    hipLaunchKernelGGL(pool_keys_kernel, dim3((a.n_kv * a.hd + 255) / 256, a.max_blocks, a.n_seq), dim3(256), 0, s, a);
     HIP_TRY(hipGetLastError());
     const dim3 grid(a.n_qb, a.n_heads, a.n_seq);
-    if (a.max_blocks <= 256)
+    if (a.max_blocks <= 64)
+        hipLaunchKernelGGL(select_blocks_kernel<1>, grid, dim3(64), 0, s, a);
+    else if (a.max_blocks <= 256)
         hipLaunchKernelGGL(select_blocks_kernel<4>, grid, dim3(64), 0, s, a);
     else if (a.max_blocks <= 1024)
         hipLaunchKernelGGL(select_blocks_kernel<16>, grid, dim3(64), 0, s, a);
