@@ -367,27 +367,25 @@ _ATTN_ARGS = struct.Struct("Pq4P10i3f0q")
 
 def _act_type(x, name: str, layout: int, shape) -> int:
     """ACT_F32 or ACT_I8 of a CUDA activation tensor that holds [rows, cols] = shape."""
-    torch = _torch
     if not x.is_cuda or not x.is_contiguous():
         raise ValueError(f"{name} must be a contiguous CUDA tensor")
-    if x.dtype == torch.float32:
-        if tuple(x.shape) != shape:
+    dt = x.dtype
+    if dt is _torch.float32:
+        if x.shape != shape:  # (a torch.Size is a tuple)
             raise ValueError(f"{name} must be {shape}")
         return ACT_F32
-    if x.dtype != torch.int8:
+    if dt is not _torch.int8:
         raise ValueError(f"{name} must be float32 or int8")
     want = t16x32_shape(*shape) if layout == LAYOUT_T16X32 else shape
-    if tuple(x.shape) != want:
+    if x.shape != want:
         raise ValueError(f"{name} must have shape {want}")
     return ACT_I8
 
 
-def _f32_ptr(x, name: str, *shapes) -> int:
-    """Address of an optional contiguous fp32 CUDA tensor of one of the shapes; 0 for None."""
-    if x is None:
-        return 0
-    if x.dtype != _torch.float32 or not x.is_cuda or not x.is_contiguous() or tuple(x.shape) not in shapes:
-        raise ValueError(f"{name} must be a contiguous CUDA float32 tensor of shape {' or '.join(map(str, shapes))}")
+def _f32_ptr(x, name: str, shape) -> int:
+    """Address of a contiguous fp32 CUDA tensor of that shape."""
+    if x.dtype is not _torch.float32 or x.shape != shape or not x.is_cuda or not x.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous CUDA float32 tensor of shape {shape}")
     return x.data_ptr()
 
 
@@ -414,30 +412,36 @@ def residual_norm(y, gamma=None, beta=None, *, norm: int = NORM_LAYER, eps: floa
     shape = rows, cols = int(shape[0]), int(shape[1])
     y_type = _act_type(y, "y", y_layout, shape)
     r_type = ACT_NONE if residual is None else _act_type(residual, "residual", r_layout, shape)
-    gate_kind = GATE_NONE
+    gate_kind, gate_ptr = GATE_NONE, 0
     if gate is not None:
-        gs = tuple(gate.shape)
+        gs = gate.shape
         gate_kind = (GATE_CHANNEL if gs == (cols,) else GATE_ELEMENT if gs == shape and cols > 1 else
                      GATE_TOKEN if gs == (rows, 1) else -1)
         if gate_kind < 0:
             raise ValueError(f"gate must be [{cols}], [{rows}, 1] or [{rows}, {cols}]")
-
-    def kept(keep):
-        return None if keep is False or keep is None else \
-            torch.empty(shape, dtype=torch.float32, device=y.device) if keep is True else keep
-
-    h, u, q = kept(keep_sum), kept(keep_norm), None
+        gate_ptr = _f32_ptr(gate, "gate", gs)
+    channels = (cols,)
+    h = u = q = None
+    if keep_sum is not False and keep_sum is not None:
+        h = torch.empty(shape, dtype=torch.float32, device=y.device) if keep_sum is True else keep_sum
+    if keep_norm is not False and keep_norm is not None:
+        u = torch.empty(shape, dtype=torch.float32, device=y.device) if keep_norm is True else keep_norm
     if out_scale is not None:
         q_shape = t16x32_shape(rows, cols) if q_layout == LAYOUT_T16X32 else shape
-        q = torch.empty(q_shape, dtype=torch.int8, device=y.device) if q_out is None else q_out
-        if q.dtype != torch.int8 or tuple(q.shape) != q_shape or not q.is_contiguous() or not q.is_cuda:
-            raise ValueError(f"q_out must be a contiguous CUDA int8 tensor of shape {q_shape}")
+        if q_out is None:
+            q = torch.empty(q_shape, dtype=torch.int8, device=y.device)
+        else:
+            q = q_out
+            if q.dtype is not torch.int8 or q.shape != q_shape or not q.is_contiguous() or not q.is_cuda:
+                raise ValueError(f"q_out must be a contiguous CUDA int8 tensor of shape {q_shape}")
     args = _NORM_ARGS.pack(
-        rows, y.data_ptr(), 0 if residual is None else residual.data_ptr(),
-        0 if gate is None else _f32_ptr(gate, "gate", tuple(gate.shape)), _f32_ptr(post_gamma, "post_gamma", (cols,)),
-        _f32_ptr(post_beta, "post_beta", (cols,)), _f32_ptr(gamma, "gamma", (cols,)), _f32_ptr(beta, "beta", (cols,)),
-        _f32_ptr(h, "keep_sum", shape), _f32_ptr(u, "keep_norm", shape), 0 if q is None else q.data_ptr(),
-        cols, y_type, y_layout, r_type, r_layout, gate_kind, post_norm, norm, q_layout,
+        rows, y.data_ptr(), 0 if residual is None else residual.data_ptr(), gate_ptr,
+        0 if post_gamma is None else _f32_ptr(post_gamma, "post_gamma", channels),
+        0 if post_beta is None else _f32_ptr(post_beta, "post_beta", channels),
+        0 if gamma is None else _f32_ptr(gamma, "gamma", channels),
+        0 if beta is None else _f32_ptr(beta, "beta", channels),
+        0 if h is None else _f32_ptr(h, "keep_sum", shape), 0 if u is None else _f32_ptr(u, "keep_norm", shape),
+        0 if q is None else q.data_ptr(), cols, y_type, y_layout, r_type, r_layout, gate_kind, post_norm, norm, q_layout,
         y_scale, r_scale, residual_scale, eps, 1.0 if out_scale is None else out_scale)
     st = load().residual_norm(args, _stream_ptr(stream))
     if st != SL_OK:
