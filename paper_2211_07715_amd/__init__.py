@@ -536,11 +536,13 @@ def select_blocks(qkv, seq_start, max_len: int, n_heads: int, head_dim: int, top
                            1.0, 1.0, 1.0)
     lib, s = load(), _stream_ptr(stream)
     size = lib.attention_select_workspace(args)
-    # (freed on the current stream: another stream's work must be told of it)
-    work = torch.empty(size, dtype=torch.uint8, device=qkv.device)
+    # from the memory of the stream that uses it, which is not handed on before that work is done
+    if stream is None:
+        work = torch.empty(size, dtype=torch.uint8, device=qkv.device)
+    else:
+        with torch.cuda.stream(stream):
+            work = torch.empty(size, dtype=torch.uint8, device=qkv.device)
     st = lib.attention_select(args, out.data_ptr(), work.data_ptr(), size, s)
-    if stream is not None:
-        work.record_stream(stream)
     if st != SL_OK:
         _check(st, "attention_select")
     return out

@@ -299,3 +299,51 @@ def test_graph_and_stream(hip):
     y = hip.attention(x, 0.04, start, 500, 2, 64, kind=1, blocks=b, stream=st)
     st.synchronize()
     assert torch.equal(y, out[1])
+
+
+def test_a_block_listed_twice_counts_twice(hip):
+    """Weights of a block's keys double, of the short last one too."""
+    import torch
+    x = _codes(np.random.default_rng(12), 150, 3 * 64)
+    xs, start = float(np.float32(0.03)), np.array([0, 150])
+    lists = np.array([[[[0, 2, 0, 2, 2], [1, 1, 0, -1, -1], [2, 2, -1, 2, 0]]]], np.int32)
+    got = hip.attention(torch.from_numpy(x).cuda(), xs, torch.tensor([0, 150], dtype=torch.int32, device="cuda"), 150, 1,
+                        64, kind=1, blocks=torch.from_numpy(lists).cuda()).cpu().numpy()
+    q, k, v = (t[:, 0] for t in ref.split_heads(x, start, 0, 1, 1, 64))
+    times = np.array([[np.sum(lists[0, 0, i // 64] == j // 64) for j in range(150)] for i in range(150)])
+    z = q @ k.T * (xs * xs / 8)
+    p = times * np.exp(z - z.max(1, keepdims=True))
+    want = (p / p.sum(1, keepdims=True)) @ v * xs
+    spread = 1.45 * float((z.max(1) - z.min(1)).max())
+    rel = 2.0 ** -23 + spread * (2.0 ** -23 + 2.0 ** -22) + 2.0 ** -20  # as in the bars above
+    assert np.abs(got - want).max() <= 128 * xs * (2 * rel + (320 / 16 + 8) * 2.0 ** -24)
+
+
+def test_select_on_two_streams(hip):
+    """Each call's workspace is its stream's: two streams that choose at once do not meet in it."""
+    import torch
+    rng = np.random.default_rng(14)
+    xs = [torch.from_numpy(_codes(rng, 4096, 3 * 2 * 64)).cuda() for _ in range(2)]
+    start = torch.tensor([0, 4096], dtype=torch.int32, device="cuda")
+    want = [hip.select_blocks(x, start, 4096, 2, 64, 8) for x in xs]
+    outs = [[torch.empty_like(want[0]) for _ in range(20)] for _ in xs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in xs]
+    for i in range(20):
+        for x, st, o in zip(xs, streams, outs):
+            hip.select_blocks(x, start, 4096, 2, 64, 8, out=o[i], stream=st)
+    torch.cuda.synchronize()
+    assert all(torch.equal(t, w) for o, w in zip(outs, want) for t in o)
+
+
+@pytest.mark.parametrize("kind", [1, 3])
+def test_growing_scores_in_every_shape(hip, kind):
+    """Keys whose scores grow to the end, so that m moves again and again, in the shapes that the sizes choose:
+    two tiles a wave, keys split over waves, and the common one; one sequence shorter than a chunk among them."""
+    rng = np.random.default_rng(21)
+    for lens, nh in (([2048] * 4, 16), ([900], 2), ([300] * 40 + [7], 4)):
+        x = _codes(rng, sum(lens), 3 * nh * 64)
+        grow = np.concatenate([np.linspace(0.02, 1.0, n) for n in lens])[:, None]
+        keys = slice(nh * 64, 2 * nh * 64)
+        x[:, keys] = np.clip(np.rint(x[:, keys] * grow * 2), -127, 127).astype(np.int8)
+        _check(hip, x, lens, nh, nh, 64, kind, x_scale=0.15)
