@@ -186,8 +186,6 @@ __global__ __launch_bounds__(64 * NW * SPLIT) __attribute__((amdgpu_waves_per_eu
     constexpr int NT = 64 * NW;
     constexpr int KN = kChunk * 2 * N, VN = kChunk / 4 * D / 4;  // a chunk's 16-byte pieces of K and 4 x 4 ones of V
     constexpr int KP = (KN + NT - 1) / NT, VP = (VN + NT - 1) / NT;  // and a thread's
-    // (the widest heads have no registers for the next chunk: it is loaded when it is written)
-    constexpr bool AHEAD = N <= 3;
     constexpr int NBUF = SPLIT == 1 ? 2 : 1;  // (one wave's reads and writes of LDS keep their order)
     static_assert(SPLIT == 1 || (NW == 1 && QT == 1), "one wave a part");
     // (the parts' O: 16 N floats a lane)
@@ -471,7 +469,7 @@ __global__ __launch_bounds__(64 * NW * SPLIT) __attribute__((amdgpu_waves_per_eu
                     from[t] = from_z(t);
                 }
                 for (;;) {
-                    if (AHEAD && b >= 0) load(b);  // (again after m has moved)
+                    if (b >= 0) load(b);  // (again after m has moved)
                     float sum[QT];
                     bool over = false;  // (no weight is over 65504 while their sum is below kMostSum)
 #pragma unroll
@@ -486,7 +484,6 @@ __global__ __launch_bounds__(64 * NW * SPLIT) __attribute__((amdgpu_waves_per_eu
                     multiply(lds + buf);
                     if (b < 0) goto done;
                     if constexpr (NBUF > 1) buf ^= BUF;
-                    if constexpr (!AHEAD) load(b);
                     stage(lds + buf);
                     b = next();
                     sync();
@@ -539,7 +536,7 @@ __global__ __launch_bounds__(64 * NW * SPLIT) __attribute__((amdgpu_waves_per_eu
             for (int w = 0; w < SPLIT; ++w)
                 sum += ls[w][n32] * __builtin_amdgcn_exp2f(-(float)(zs[w][n32] - zmin) * a.c2);
             __syncthreads();
-            const float g = sum > 0.0f ? a.xs / sum : 0.0f;
+            const float g = sum > 0.0f ? a.xs / sum * (a.y_f32 ? 1.0f : a.inv_so) : 0.0f;
             const int32_t qi = query(0);
             const int64_t tok = (int64_t)sp.first + qi;
 #pragma unroll
@@ -551,16 +548,15 @@ __global__ __launch_bounds__(64 * NW * SPLIT) __attribute__((amdgpu_waves_per_eu
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
                         v[j] += reinterpret_cast<const float *>(all_lds)[w * (64 * 16 * N) + (first + j) * 64 + lane];
-                v *= g;
                 const int32_t c = 16 * N * here(half) + first;
                 if (qi < 0 || c >= a.hd) continue;
                 if (a.y_f32)
-                    *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(a.y) + tok * (a.n_heads * a.hd) + head * a.hd + c) = v;
+                    *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(a.y) + tok * (a.n_heads * a.hd) + head * a.hd + c) = v * g;
                 else
                     *reinterpret_cast<uint32_t *>(reinterpret_cast<int8_t *>(a.y) +
                                                   at(tok, head * a.hd + c, a.n_heads * a.hd, a.y_cb)) =
-                        pack_bytes(requant_bits(v[0], a.inv_so), requant_bits(v[1], a.inv_so),
-                                   requant_bits(v[2], a.inv_so), requant_bits(v[3], a.inv_so));
+                        pack_bytes(requant_bits(v[0], g), requant_bits(v[1], g), requant_bits(v[2], g),
+                                   requant_bits(v[3], g));
             }
             __syncthreads();
             continue;
@@ -568,7 +564,8 @@ __global__ __launch_bounds__(64 * NW * SPLIT) __attribute__((amdgpu_waves_per_eu
         // a lane half holds features 16 N half .. 16 N half + 16 N - 1 of its query
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
-            const float sum = pair_sum(l[t]), f = sum > 0.0f ? a.xs / sum : 0.0f;
+            const float sum = pair_sum(l[t]);
+            const float f = sum > 0.0f ? a.xs / sum * (a.y_f32 ? 1.0f : a.inv_so) : 0.0f;
             const int32_t qi = query(t);
             if (qi < 0) continue;
             const int64_t tok = (int64_t)sp.first + qi;
@@ -589,8 +586,8 @@ __global__ __launch_bounds__(64 * NW * SPLIT) __attribute__((amdgpu_waves_per_eu
 #pragma unroll
                     for (int i = 0; i < 16; i += 4)
                         w[i / 4] = (int)pack_bytes(
-                            requant_bits(o[t][d][i] * f, a.inv_so), requant_bits(o[t][d][i + 1] * f, a.inv_so),
-                            requant_bits(o[t][d][i + 2] * f, a.inv_so), requant_bits(o[t][d][i + 3] * f, a.inv_so));
+                            requant_bits(o[t][d][i], f), requant_bits(o[t][d][i + 1], f),
+                            requant_bits(o[t][d][i + 2], f), requant_bits(o[t][d][i + 3], f));
                     const int32_t c = 16 * N * h2 + 16 * d;
                     if (c < a.hd)
                         *reinterpret_cast<i32x4 *>(reinterpret_cast<int8_t *>(a.y) +
