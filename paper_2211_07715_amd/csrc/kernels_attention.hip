@@ -65,7 +65,7 @@ struct AttnArgs {
     int64_t m;
     int64_t n_items;
     int32_t n_seq, tiles, tq, n_heads, n_kv, hd, cols, x_cb, y_cb;
-    int32_t top_k, n_qb, y_f32;
+    int32_t top_k, n_qb, halvings, y_f32;  // tq << halvings: queries of a list
     float c2, k2, inv_so, xs;
 };
 
@@ -417,8 +417,9 @@ __global__ __launch_bounds__(64 * NW * SPLIT) __attribute__((amdgpu_waves_per_eu
         // Whole chunks first, then the sequence's short last one. With lists:
         // 64 numbers at a time, one a lane; those of whole chunks as a mask.
         const int32_t whole = sp.keys / kChunk, rest = sp.keys % kChunk;
-        const int32_t steps = LISTS ? (qt < a.n_qb ? a.top_k : 0) : whole;
-        const int32_t *list = a.blocks + (((int64_t)seq * a.n_heads + head) * a.n_qb + qt) * a.top_k;
+        const int32_t steps = LISTS ? (qt >> a.halvings < a.n_qb ? a.top_k : 0) : whole;
+        const int32_t *list =
+            a.blocks + (((int64_t)seq * a.n_heads + head) * a.n_qb + (qt >> a.halvings)) * a.top_k;
         int32_t at_step = LISTS ? 0 : part, mine = -1, tails = !LISTS && rest && (SPLIT == 1 || whole % SPLIT == part);
         uint64_t left = 0;
         const uint64_t ours = SPLIT == 1 ? ~0ull : 0x1111111111111111ull << part;
@@ -618,20 +619,30 @@ sl_status launch_shape(AttnArgs &a, int32_t tq, int32_t max_len, hipStream_t s)
 template <int N>
 sl_status launch_head(AttnArgs &a, const sl_attention_args &args, hipStream_t s)
 {
-    const int32_t n = args.max_len, qb = args.query_block;
-    if (!args.blocks) {
-        const int64_t heads = (int64_t)args.n_heads * args.n_seq;
-        const int64_t items = heads * ((n + 127) / 128), wide = heads * ((n + 255) / 256);
-        if constexpr (N <= 2) {
-            // Two tiles a wave stage and read a chunk half as often, where 256-query items still fill the CUs twice and
-            // the last one of a sequence is a small part: 8192 tokens of 16 heads 365 us against 393, 8 x 2048 of 12
-            // heads 148 against 155; 4096 tokens of 12 heads (192 items) 87 against 80.
-            if (n >= 1024 && wide >= 512) return launch_shape<N, 2, 4, 1, false>(a, 256, n, s);
-            // Keys split over the waves, where 128-query items leave most CUs without one: 384 tokens of 12 heads
-            // 8.9 us against 10.8, 1024 tokens 17.8 against 21.7; 4 x 384 tokens (144 items) 16.7 against 11.2, and
-            // 128 tokens (two chunks) 7.0 against 6.5.
-            if (n >= 256 && items <= 96) return launch_shape<N, 1, 1, 4, false>(a, 32, n, s);
+    const int32_t n = args.max_len, qb = args.query_block, tq = args.blocks ? std::min(qb, 32) : 32;
+    const int64_t heads = (int64_t)args.n_heads * args.n_seq;
+    a.halvings = 0;
+    if constexpr (N <= 2) {
+        // Keys split over the waves, where 32 queries a workgroup (16 with query_block 16) make two workgroups a CU at
+        // most; twice that for long sequences of heads to 32 features. Dense: 384 tokens of 12 heads 8.6 us against
+        // 10.7, 1024 of 16 heads 17.7 against 21.7, 4096 of 4 heads 46 against 68; 2048 of 12 heads (768 workgroups) 39
+        // against 38, 1024 of 24 heads 26 against 22, and 128 tokens (two chunks) 7.0 against 6.5. Heads of 32 features:
+        // 1024 tokens of 32 heads (1024 workgroups) 18 against 21, 256 of 128 heads 11.0 against 9.1. Lists at 4096 tokens
+        // of 4 heads (512 workgroups) with query_block 64: 16 blocks 18 against 26, 4 blocks 10.2 against 11.1; of 8
+        // heads with 128: 16 blocks 32 against 24.
+        const int64_t groups = heads * ((n + tq - 1) / tq), most = N == 1 && !args.blocks && n >= 1024 ? 1024 : 512;
+        if (groups <= most && (args.blocks ? args.top_k >= 4 : n >= 256)) {
+            if (!args.blocks) return launch_shape<N, 1, 1, 4, false>(a, 32, n, s);
+            a.halvings = __builtin_ctz(qb / tq);
+            return launch_shape<N, 1, 1, 4, true>(a, tq, n, s);
         }
+    }
+    if (!args.blocks) {
+        // Two tiles a wave stage and read a chunk half as often, where 256-query items still fill the CUs twice and the
+        // last one of a sequence is a small part: 8192 tokens of 16 heads 365 us against 393, 8 x 2048 of 12 heads 148
+        // against 155; 4096 tokens of 12 heads (192 items) 87 against 80.
+        if constexpr (N <= 2)
+            if (n >= 1024 && heads * ((n + 255) / 256) >= 512) return launch_shape<N, 2, 4, 1, false>(a, 256, n, s);
         return launch_shape<N, 1, 4, 1, false>(a, 128, n, s);
     }
     if constexpr (N <= 2) {

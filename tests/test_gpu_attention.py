@@ -347,3 +347,20 @@ def test_growing_scores_in_every_shape(hip, kind):
         keys = slice(nh * 64, 2 * nh * 64)
         x[:, keys] = np.clip(np.rint(x[:, keys] * grow * 2), -127, 127).astype(np.int8)
         _check(hip, x, lens, nh, nh, 64, kind, x_scale=0.15)
+
+
+@pytest.mark.parametrize("qb", [16, 32, 64, 128])
+@pytest.mark.parametrize("hd", [32, 64])
+def test_lists_in_every_shape(hip, qb, hd):
+    """Few workgroups (a list's keys split over waves) and many, with lists of numbers out of order, gaps and a short
+    last block, and with scores that grow."""
+    rng = np.random.default_rng(qb + hd)
+    for lens, nh in (([450, 0, 70], 2), ([200, 65, 1, 130] * 40, 4)):
+        x = _codes(rng, sum(lens), 3 * nh * hd)
+        keys = slice(nh * hd, 2 * nh * hd)
+        grow = np.concatenate([np.linspace(0.1, 1.0, n) for n in lens])[:, None]
+        x[:, keys] = np.clip(np.rint(x[:, keys] * grow * 2), -127, 127).astype(np.int8)
+        for top_k in (3, 6):
+            order = rng.permuted(np.tile(np.arange(8), (len(lens), nh, -(-max(lens) // qb), 1)), axis=-1)
+            lists = np.where(order < 7, order, -1)[..., :top_k]
+            _check(hip, x, lens, nh, nh, hd, 1 if top_k == 3 else 3, x_scale=0.1, lists=lists, qb=qb)
