@@ -176,9 +176,12 @@ __device__ __forceinline__ int vswap(int row) { return (row >> 1) & 7; }  // val
 //
 // At most 256 registers (two waves a SIMD; three for the shape of most calls), so
 // that the accumulators are ordinary registers, which the exponentials read
-// without a copy.
+// without a copy. One wave that brings in whole chunks of a head of more than 64
+// features takes more (one wave a SIMD).
 template <int N, int QT, int NW, int SPLIT, bool LISTS>
-__global__ __launch_bounds__(64 * NW * SPLIT) __attribute__((amdgpu_waves_per_eu(N <= 2 && QT == 1 && NW == 4 ? 3 : 2))) void attention_kernel(const AttnArgs a)
+__global__ __launch_bounds__(64 * NW * SPLIT)
+__attribute__((amdgpu_waves_per_eu(N <= 2 && QT == 1 && NW == 4 ? 3 : N > 2 && NW == 1 ? 1 : 2)))
+void attention_kernel(const AttnArgs a)
 {
     constexpr int D = 32 * N;
     constexpr int VS = 2 * kChunk;             // LDS bytes of a feature of V (of a key: D)
@@ -622,20 +625,20 @@ sl_status launch_head(AttnArgs &a, const sl_attention_args &args, hipStream_t s)
     const int32_t n = args.max_len, qb = args.query_block, tq = args.blocks ? std::min(qb, 32) : 32;
     const int64_t heads = (int64_t)args.n_heads * args.n_seq;
     a.halvings = 0;
-    if constexpr (N <= 2) {
-        // Keys split over the waves, where 32 queries a workgroup (16 with query_block 16) make two workgroups a CU at
-        // most; twice that for long sequences of heads to 32 features. Dense: 384 tokens of 12 heads 8.6 us against
-        // 10.7, 1024 of 16 heads 17.7 against 21.7, 4096 of 4 heads 46 against 68; 2048 of 12 heads (768 workgroups) 39
-        // against 38, 1024 of 24 heads 26 against 22, and 128 tokens (two chunks) 7.0 against 6.5. Heads of 32 features:
-        // 1024 tokens of 32 heads (1024 workgroups) 18 against 21, 256 of 128 heads 11.0 against 9.1. Lists at 4096 tokens
-        // of 4 heads (512 workgroups) with query_block 64: 16 blocks 18 against 26, 4 blocks 10.2 against 11.1; of 8
-        // heads with 128: 16 blocks 32 against 24.
-        const int64_t groups = heads * ((n + tq - 1) / tq), most = N == 1 && !args.blocks && n >= 1024 ? 1024 : 512;
-        if (groups <= most && (args.blocks ? args.top_k >= 4 : n >= 256)) {
-            if (!args.blocks) return launch_shape<N, 1, 1, 4, false>(a, 32, n, s);
-            a.halvings = __builtin_ctz(qb / tq);
-            return launch_shape<N, 1, 1, 4, true>(a, tq, n, s);
-        }
+    // Keys split over the waves, where 32 queries a workgroup (16 with query_block 16) make no more workgroups than the
+    // CUs hold at once: two each, one of heads over 64 features; four in long sequences of heads to 32. Dense: 384 tokens
+    // of 12 heads 8.6 us against 10.7, 1024 of 16 heads 17.7 against 21.7, 4096 of 4 heads 46 against 68; 2048 of 12
+    // heads (768 workgroups) 39 against 38, 1024 of 24 heads 26 against 22, and 128 tokens (two chunks) 7.0 against 6.5.
+    // Heads of 32 features: 1024 tokens of 32 heads (1024 workgroups) 18 against 21, 256 of 128 heads 11.0 against 9.1.
+    // Heads of 128: 4096 tokens of 2 heads (256 workgroups) 50 against 107, 1024 of 12 heads 37 against 34. Lists at 4096
+    // tokens of 4 heads (512 workgroups) with query_block 64: 16 blocks 18 against 26, 4 blocks 10.2 against 11.1; of 8
+    // heads with 128: 16 blocks 32 against 24.
+    const int64_t groups = heads * ((n + tq - 1) / tq);
+    const int64_t most = N > 2 ? 256 : N == 1 && !args.blocks && n >= 1024 ? 1024 : 512;
+    if (groups <= most && (args.blocks ? args.top_k >= 4 : n >= 256)) {
+        if (!args.blocks) return launch_shape<N, 1, 1, 4, false>(a, 32, n, s);
+        a.halvings = __builtin_ctz(qb / tq);
+        return launch_shape<N, 1, 1, 4, true>(a, tq, n, s);
     }
     if (!args.blocks) {
         // Two tiles a wave stage and read a chunk half as often, where 256-query items still fill the CUs twice and the
@@ -645,12 +648,14 @@ sl_status launch_head(AttnArgs &a, const sl_attention_args &args, hipStream_t s)
             if (n >= 1024 && heads * ((n + 255) / 256) >= 512) return launch_shape<N, 2, 4, 1, false>(a, 256, n, s);
         return launch_shape<N, 1, 4, 1, false>(a, 128, n, s);
     }
-    if constexpr (N <= 2) {
+    // As many waves as have queries, against four, 16 blocks at 8192 tokens of 12 heads: of 64 features with query_block
+    // 64 70 us against 78, of 96 features 89 against 108, with 32 108 against 173, with 16 205 against 340. (One or two
+    // waves would hold the chunk of a head of 128 in too many registers: 8 heads at 4096 tokens with query_block 32 90
+    // against 66.)
+    if constexpr (N <= 3) {
         if (qb <= 32) return launch_shape<N, 1, 1, 1, true>(a, qb, n, s);
-        // (four waves, two of them without queries: 214 us against 191 for 32 of 16384 tokens' blocks)
         if (qb == 64) return launch_shape<N, 1, 2, 1, true>(a, qb, n, s);
     }
-    // (one or two waves would hold a wide head's chunk in too many registers)
     return launch_shape<N, 1, 4, 1, true>(a, qb, n, s);
 }
 

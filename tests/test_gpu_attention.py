@@ -350,7 +350,7 @@ def test_growing_scores_in_every_shape(hip, kind):
 
 
 @pytest.mark.parametrize("qb", [16, 32, 64, 128])
-@pytest.mark.parametrize("hd", [32, 64])
+@pytest.mark.parametrize("hd", [32, 64, 96, 128])
 def test_lists_in_every_shape(hip, qb, hd):
     """Few workgroups (a list's keys split over waves) and many, with lists of numbers out of order, gaps and a short
     last block, and with scores that grow."""
@@ -364,3 +364,15 @@ def test_lists_in_every_shape(hip, qb, hd):
             order = rng.permuted(np.tile(np.arange(8), (len(lens), nh, -(-max(lens) // qb), 1)), axis=-1)
             lists = np.where(order < 7, order, -1)[..., :top_k]
             _check(hip, x, lens, nh, nh, hd, 1 if top_k == 3 else 3, x_scale=0.1, lists=lists, qb=qb)
+
+
+@pytest.mark.parametrize("hd", [32, 96, 128])
+def test_growing_scores_in_every_shape_of_other_heads(hip, hd):
+    """Few long sequences (keys split over waves), many, and one with too few keys for all of the parts."""
+    rng = np.random.default_rng(hd)
+    for lens, nh, kind in (([900], 2, 1), ([2100], 3, 3), ([300] * 40 + [7], 4, 1), ([300, 20], 1, 3)):
+        x = _codes(rng, sum(lens), 3 * nh * hd)
+        grow = np.concatenate([np.linspace(0.02, 1.0, n) for n in lens])[:, None]
+        keys = slice(nh * hd, 2 * nh * hd)
+        x[:, keys] = np.clip(np.rint(x[:, keys] * grow * 2), -127, 127).astype(np.int8)
+        _check(hip, x, lens, nh, nh, hd, kind, x_scale=0.1)
