@@ -95,6 +95,12 @@ __device__ __forceinline__ int here(int lane)
     return lane;
 }
 
+// 16 bytes a lane to 64 pieces of LDS in order of the lanes, from `to` on; landed once the wave's loads are waited for.
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t x, char *to, uint32_t offset, uint32_t more)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(x, (lds_void *)to, 16, offset, more, 0, 0);
+}
+
 // Of the two lanes that hold a query's scores.
 __device__ __forceinline__ int pair_max(int v)
 {
@@ -167,8 +173,12 @@ __device__ __forceinline__ int vswap(int row) { return (row >> 1) & 7; }  // val
 
 // N: 32-feature tiles of a head (head_dim <= 32 N); NW: waves, of QT tiles of 32
 // queries each, which share the chunk of keys and values in LDS. Two
-// buffers: the next chunk is loaded into registers while one is multiplied, and
-// written to the other buffer (V transposed) before the barrier.
+// buffers: while one chunk is multiplied, the next one's K is loaded into the
+// other buffer and its V into registers, which are written there (transposed)
+// before the barrier. That K takes no registers lets lists of 64 queries have
+// three waves a SIMD: 32 blocks at 16384 tokens of 12 heads 185 us against 211.
+// One wave has one buffer and K in registers (twice the workgroups in LDS: 16
+// blocks at 8192 tokens of 12 heads, query_block 32, 66 us against 72).
 //
 // SPLIT > 1 (NW is 1 then): a workgroup is SPLIT waves on the same queries, each
 // with every SPLIT-th chunk in a buffer of its own and no barrier until their m,
@@ -180,7 +190,7 @@ __device__ __forceinline__ int vswap(int row) { return (row >> 1) & 7; }  // val
 // features takes more (one wave a SIMD).
 template <int N, int QT, int NW, int SPLIT, bool LISTS>
 __global__ __launch_bounds__(64 * NW * SPLIT)
-__attribute__((amdgpu_waves_per_eu(N <= 2 && QT == 1 && NW == 4 ? 3 : N > 2 && NW == 1 ? 1 : 2)))
+__attribute__((amdgpu_waves_per_eu(N <= 2 && QT == 1 && NW >= 2 ? 3 : N > 2 && NW == 1 ? 1 : 2)))
 void attention_kernel(const AttnArgs a)
 {
     constexpr int D = 32 * N;
@@ -189,8 +199,9 @@ void attention_kernel(const AttnArgs a)
     constexpr int NT = 64 * NW;
     constexpr int KN = kChunk * 2 * N, VN = kChunk / 4 * D / 4;  // a chunk's 16-byte pieces of K and 4 x 4 ones of V
     constexpr int KP = (KN + NT - 1) / NT, VP = (VN + NT - 1) / NT;  // and a thread's
-    constexpr int NBUF = SPLIT == 1 ? 2 : 1;  // (one wave's reads and writes of LDS keep their order)
+    constexpr int NBUF = NW > 1 ? 2 : 1;  // (one wave's reads and writes of LDS keep their order)
     static_assert(SPLIT == 1 || (NW == 1 && QT == 1), "one wave a part");
+    constexpr bool DIRECT = NBUF > 1;  // K goes to LDS without registers
     // (the parts' O: 16 N floats a lane)
     constexpr int LDS = SPLIT * std::max(NBUF * BUF, SPLIT > 1 ? 64 * 64 * N : 0);
     __shared__ __attribute__((aligned(16))) char all_lds[LDS];
@@ -198,7 +209,7 @@ void attention_kernel(const AttnArgs a)
     const int part = SPLIT > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0;
     char *lds = all_lds + part * (NBUF * BUF);
     const auto sync = [] {
-        if constexpr (SPLIT == 1)
+        if constexpr (NW > 1)
             __syncthreads();
         else
             asm volatile("" ::: "memory");
@@ -220,7 +231,7 @@ void attention_kernel(const AttnArgs a)
     const auto kpiece = [&](int i, int &key, int &d) {
         const int p = tid + i * NT;
         key = p / (2 * N) % kChunk;
-        d = p % (2 * N) * 16;
+        d = (p % (2 * N) ^ (DIRECT ? kswap<N>(key) : 0)) * 16;
     };
     const auto vpiece = [&](int i, int &key, int &d) {
         const int p = tid + i * NT;  // (8 lanes: 32 keys of 4 features, whose stores fill 64 bytes of LDS)
@@ -261,35 +272,53 @@ void attention_kernel(const AttnArgs a)
     }
     i32x4 kreg[KP];
     uint32_t vreg[VP][4];
-    const auto load = [&](int32_t b) __attribute__((always_inline)) {
+    // Where a thread's pieces are the same features of keys KSTEP (V: 32) apart, one offset serves them in a whole chunk.
+    constexpr int KSTEP = NT % (2 * N) == 0 && NT / (2 * N) % 16 == 0 ? NT / (2 * N) : 0;
+    constexpr bool VHALF = VP == 2 && NT == 2 * D;
+    const int32_t group = rows.cb ? rows.cb * 512 : 16 * rows.cols;  // bytes of 16 keys
+    const auto load = [&](int32_t b, bool full, char *buf) __attribute__((always_inline)) {
         // (the offsets are in bounds: the resource only spares the lanes 64-bit addresses)
         const auto x = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(rows.base + b * rows.chunk), 0, 0x7fffffff,
                                                          kRsrcWord3);
 #pragma unroll
-        for (int i = 0; i < KP; ++i)
-            kreg[i] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(x, koff[i], 0, 0));
+        for (int i = 0; i < KP; ++i) {
+            const bool step = KSTEP && full;
+            const int32_t more = step ? i * (KSTEP / 16) * group : 0;
+            const int first = __builtin_amdgcn_readfirstlane(tid) + i * NT;
+            if constexpr (DIRECT) {
+                if (KP * NT == KN || first < KN)
+                    load_to_lds(x, buf + 16 * first, koff[step ? 0 : i], more);
+            } else {
+                kreg[i] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(x, koff[step ? 0 : i], more, 0));
+            }
+        }
 #pragma unroll
         for (int i = 0; i < VP; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) vreg[i][j] = __builtin_amdgcn_raw_buffer_load_b32(x, voff[i][j], 0, 0);
+            for (int j = 0; j < 4; ++j) {
+                const bool step = VHALF && full;
+                vreg[i][j] = __builtin_amdgcn_raw_buffer_load_b32(x, voff[step ? 0 : i][j], step ? i * 2 * group : 0, 0);
+            }
     };
     const auto stage = [&](char *buf) {
 #pragma unroll
         for (int i = 0; i < KP; ++i)
-            if (KP * NT == KN || tid + i * NT < KN) *reinterpret_cast<i32x4 *>(buf + kdst[i]) = kreg[i];
+            if (!DIRECT && (KP * NT == KN || tid + i * NT < KN)) *reinterpret_cast<i32x4 *>(buf + (KSTEP ? kdst[0] + i * KSTEP * D : kdst[i])) = kreg[i];
 #pragma unroll
         for (int i = 0; i < VP; ++i) {
             if (VP * NT == VN || tid + i * NT < VN) {
                 u32x2 out[4];
                 transpose_to_f16(vreg[i], out);
                 // (of rows 4 x .. 4 x + 3, the last two have the lowest bit of the swap set)
-                char *to = buf + vdst[i], *to2 = buf + (vdst[i] ^ 16);
+                const uint32_t dst = VHALF ? vdst[0] ^ (64 * i) : vdst[i];
+                char *to = buf + dst, *to2 = buf + (dst ^ 16);
                 *reinterpret_cast<u32x2 *>(to) = out[0];
                 *reinterpret_cast<u32x2 *>(to + VS) = out[1];
                 *reinterpret_cast<u32x2 *>(to2 + 2 * VS) = out[2];
                 *reinterpret_cast<u32x2 *>(to2 + 3 * VS) = out[3];
             }
         }
+        if constexpr (DIRECT) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     };
 
     for (int32_t qt = tile; (int64_t)qt * a.tq < sp.n; qt += a.tiles) {
@@ -449,14 +478,14 @@ void attention_kernel(const AttnArgs a)
         i32x16 sc[2];
         int32_t b = next();
         if (b >= 0) {
-            load(b);
+            load(b, true, lds);
             stage(lds);
             b = next();
             sync();
             int32_t buf = 0;
             if (wave * 32 * QT >= a.tq) {  // a wave without queries only brings chunks in
                 while (b >= 0) {
-                    load(b);
+                    load(b, true, lds + (buf ^ BUF));
                     buf ^= BUF;
                     stage(lds + buf);
                     b = next();
@@ -473,7 +502,7 @@ void attention_kernel(const AttnArgs a)
                     from[t] = from_z(t);
                 }
                 for (;;) {
-                    if (b >= 0) load(b);  // (again after m has moved)
+                    if (b >= 0) load(b, true, lds + (buf ^ BUF));  // (again after m has moved)
                     float sum[QT];
                     bool over = false;  // (no weight is over 65504 while their sum is below kMostSum)
 #pragma unroll
@@ -498,7 +527,7 @@ void attention_kernel(const AttnArgs a)
         }
         if (tails > 0) {
             offsets(rest);
-            load(whole);
+            load(whole, false, lds);
             stage(lds);
             sync();
             for (int32_t i = 0; i < tails; ++i) {
@@ -648,10 +677,10 @@ sl_status launch_head(AttnArgs &a, const sl_attention_args &args, hipStream_t s)
             if (n >= 1024 && heads * ((n + 255) / 256) >= 512) return launch_shape<N, 2, 4, 1, false>(a, 256, n, s);
         return launch_shape<N, 1, 4, 1, false>(a, 128, n, s);
     }
-    // As many waves as have queries, against four, 16 blocks at 8192 tokens of 12 heads: of 64 features with query_block
-    // 64 70 us against 78, of 96 features 89 against 108, with 32 108 against 173, with 16 205 against 340. (One or two
-    // waves would hold the chunk of a head of 128 in too many registers: 8 heads at 4096 tokens with query_block 32 90
-    // against 66.)
+    // As many waves as have queries, against four, 16 blocks at 8192 tokens of 12 heads with query_block 64, 32 and 16:
+    // of 64 features 51, 73 and 138 us against 63, 86 and 173, of 96 features 83, 105 and 200 against 103, 163 and 322.
+    // (One or two waves would hold the chunk of a head of 128 in too many registers: 8 heads at 4096 tokens with
+    // query_block 32 90 against 66.)
     if constexpr (N <= 3) {
         if (qb <= 32) return launch_shape<N, 1, 1, 1, true>(a, qb, n, s);
         if (qb == 64) return launch_shape<N, 1, 2, 1, true>(a, qb, n, s);
