@@ -25,6 +25,12 @@
 // factor of 2^8, which 16-bit P leaves room for: it moves, and l and O are
 // rescaled, outside the loop over chunks, which is left for that and entered
 // again (a branch inside would make the compiler copy every accumulator).
+//
+// Measured, 4 operations a score and feature: 128 x 384 tokens of 12 heads of 64
+// 110 us (527 TOP/s; vector instructions issue 86 % of the time, matrix ones run
+// 35 %), 8192 tokens of 16 heads on 4 374 us (735 TOP/s; 76 %, 42 %), 32 blocks
+// at 16384 tokens of 12 heads 179 us (576 TOP/s; 77 %, 36 %), 32 x 128 tokens 8.6
+// us, 128 tokens 6.4 us.
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -700,7 +706,8 @@ struct SelectArgs {
 };
 
 // Pooled keys: one wave a key block and 64 features of the keys, 4 features a
-// lane, and every 4th key; all 16 loads of a lane are in flight together.
+// lane, and every 4th key; all 16 loads of a lane are in flight together (16384
+// tokens of 12 heads of 64: 5.1 us, 2.5 TB/s).
 __global__ __launch_bounds__(256) void pool_keys_kernel(const SelectArgs a)
 {
     const int32_t seq = blockIdx.z, b = blockIdx.y, lane = threadIdx.x & 63;
@@ -741,7 +748,7 @@ __global__ __launch_bounds__(256) void pool_keys_kernel(const SelectArgs a)
 // products are summed 8 at a time in 32 bits (8 * 2^14 * 2^13 < 2^31), then in
 // 64. The top_k-th largest is found bit by bit, by counting. (Bound by the
 // latency of its steps: four query blocks a wave, which read the pooled keys a
-// quarter as often, took 29 us against 17 at 16384 tokens.)
+// quarter as often, took 29 us against 17 at 16384 tokens; now 13.8.)
 template <int VPL>
 __global__ __launch_bounds__(64) void select_blocks_kernel(const SelectArgs a)
 {
