@@ -192,3 +192,18 @@ def test_graph_and_stream(hip):
         torch.cuda.synchronize()
         want = hip.residual_norm(y, residual=r, keep_sum=True, keep_norm=True, out_scale=0.03)
         assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+@pytest.mark.parametrize("n", [513, 600, 768, 769, 1001, 1024])
+def test_widths_of_many_rows(hip, n):
+    """More rows than a row is given four waves for, and the last of those."""
+    for i, m in enumerate((2048, 2049, 2103)):
+        _run(hip, m, n, i == 1, ("f32", "i8", "none")[i], (0, 1, 2)[i], ("none", "channel", "element")[i],
+             (1, 2, 1)[i], "huq", ((0, 0, 0), (1, 1, 1), (0, 0, 1))[i], seed=i)
+
+
+@pytest.mark.parametrize("n", [2049, 2560, 3013, 3071, 3073, 3999, 4095])
+def test_widths_between_2048_and_4096(hip, n):
+    for i, m in enumerate((1, 6, 19)):
+        _run(hip, m, n, i == 1, ("f32", "i8", "none")[i], (0, 1, 2)[i], ("none", "channel", "element")[i],
+             (1, 2, 1)[i], "huq", ((0, 0, 0), (1, 1, 1), (0, 0, 1))[i], seed=i)
