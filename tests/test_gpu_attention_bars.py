@@ -1,0 +1,59 @@
+"""GPU tests of attention_run against its definition in 64 bits with the bars of
+attention_bars.py, the same for fp32 results and int8 codes."""
+import numpy as np
+import pytest
+
+import attention_bars as bars
+
+pytestmark = pytest.mark.gpu
+T = 1  # LAYOUT_T16X32
+
+
+def check(hip, x, lens, nh, nkv, hd, kind, xl=0, yl=0, x_scale=0.04, sm=None, key_len=None, lists=None, qb=64,
+          max_len=None, step=bars.STEP):
+    import torch
+    m, start = len(x), bars.starts(lens)
+    dev = lambda a: None if a is None else torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).cuda()  # noqa: E731
+    xs = float(np.float32(x_scale))
+    scale = float(np.float32(hd ** -0.5 if sm is None else sm))
+    want, bar = bars.attention(x, xs, start, nh, nkv, hd, scale, key_len, lists, qb, step)
+    so = bars.output_scale(want)
+    longest = max(lens) if max_len is None else max_len
+    print(f"attention {list(lens)[:8]} heads={nh}/{nkv}x{hd} kind={kind} layouts=({xl},{yl}) qb={qb}", flush=True)
+    xd = torch.from_numpy(np.ascontiguousarray(hip.to_t16x32(x, fill=77) if xl == T else x)).cuda()
+    y = hip.attention(xd, xs, dev(start), longest, nh, hd, n_kv_heads=nkv, softmax_scale=sm, key_len=dev(key_len),
+                      kind=kind, out_scale=so, blocks=dev(lists), query_block=qb, x_layout=xl, y_layout=yl, m_tokens=m)
+    torch.cuda.synchronize()
+    got = y.cpu().numpy()
+    got = hip.from_t16x32(got, m, nh * hd) if yl == T else got
+    used = start[-1]
+    bars.judge(got[:used], want[:used], bar[:used], so if kind == 3 else None)
+    return got
+
+
+@pytest.mark.parametrize("kind", [1, 3])
+@pytest.mark.parametrize("hd", [16, 32, 48, 64, 80, 96, 112, 128])
+def test_every_head_size(hip, hd, kind):
+    rng = np.random.default_rng([hd, kind])
+    lens = [128, 1, 65, 0, 200, 64, 385, 31]
+    for nh, nkv, xl in ((4, 4, 0), (6, 2, T)):
+        check(hip, bars.codes(rng, sum(lens), (nh + 2 * nkv) * hd), lens, nh, nkv, hd, kind, xl)
+
+
+@pytest.mark.parametrize("kind", [1, 3])
+@pytest.mark.parametrize("b,n,nh", [(32, 128, 4), (3, 384, 12), (1, 1000, 2), (1, 4097, 1), (40, 257, 4)])
+def test_batches(hip, b, n, nh, kind):
+    rng = np.random.default_rng([b, n])
+    check(hip, bars.codes(rng, b * n, 3 * nh * 64), [n] * b, nh, nh, 64, kind, T, T if kind == 3 else 0)
+
+
+@pytest.mark.parametrize("qb", [16, 32, 64, 128])
+def test_lists(hip, qb):
+    rng = np.random.default_rng(qb)
+    lens, keys, nh = [700, 1, 64, 0, 333, 129], [700, 1, 0, 0, 300, 65], 3
+    blocks = -(-700 // 64)
+    lists = rng.permuted(np.tile(np.arange(blocks), (len(lens), nh, -(-700 // qb), 1)), axis=-1)[..., :5]
+    for hd in (32, 64, 96, 128):
+        x = bars.codes(rng, sum(lens), 3 * nh * hd)
+        for kind in (1, 3):
+            check(hip, x, lens, nh, nh, hd, kind, key_len=keys, lists=lists, qb=qb)
