@@ -394,12 +394,15 @@ int32_t sl_abi_version(void);
 
 /*
  * Thread-local text naming the kernel and workgroup shape of the last
- * successful sparse_linear_run / sparse_linear_run_layout on this thread
- * ("" before the first): "split st,nt kw=K wpw=W" (split reduction, for
+ * successful sparse_linear_run / sparse_linear_run_layout / attention_run that
+ * launched one on this thread ("" before the first): "split st,nt kw=K wpw=W" (split reduction, for
  * few tokens), "panel nt,st,nwv,r" (weight-stationary), "tile tokens,nt" (long
  * reductions), "direct st,nt,wm,d" or "staged st,ct,wm,wn,d", followed by " gelu=erf" when an
  * int8 GELU epilogue evaluated erf because its output scale (below about
- * 0.015) admits no step table. For tests and tuning; the text is valid until
+ * 0.015) admits no step table; "attention features,tiles,waves,split" (features
+ * that a head is padded to, tiles of 32 queries a wave, waves that share a chunk
+ * of keys, parts that the keys are split into), followed by " lists" with blocks.
+ * For tests and tuning; the text is valid until
  * the next run on this thread.
  */
 const char *sl_last_path(void);

@@ -35,6 +35,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <string>
 
 #include "encoder.h"
 #include "sl_device.h"
@@ -651,6 +652,10 @@ sl_status launch_shape(AttnArgs &a, int32_t tq, int32_t max_len, hipStream_t s)
     hipLaunchKernelGGL((attention_kernel<N, QT, NW, SPLIT, LISTS>), dim3((uint32_t)a.n_items),
                        dim3(64 * NW * SPLIT), 0, s, a);
     HIP_TRY(hipGetLastError());
+    // (formatted once: this is on the path of every call)
+    static const std::string name = "attention " + std::to_string(32 * N) + "," + std::to_string(QT) + "," +
+                                    std::to_string(NW) + "," + std::to_string(SPLIT) + (LISTS ? " lists" : "");
+    set_last_path("%s", name.c_str());
     return SL_OK;
 }
 

@@ -10,7 +10,7 @@ T = 1  # LAYOUT_T16X32
 
 
 def check(hip, x, lens, nh, nkv, hd, kind, xl=0, yl=0, x_scale=0.04, sm=None, key_len=None, lists=None, qb=64,
-          max_len=None, step=bars.STEP):
+          max_len=None, step=bars.STEP, path=None):
     import torch
     m, start = len(x), bars.starts(lens)
     dev = lambda a: None if a is None else torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).cuda()  # noqa: E731
@@ -24,6 +24,8 @@ def check(hip, x, lens, nh, nkv, hd, kind, xl=0, yl=0, x_scale=0.04, sm=None, ke
     y = hip.attention(xd, xs, dev(start), longest, nh, hd, n_kv_heads=nkv, softmax_scale=sm, key_len=dev(key_len),
                       kind=kind, out_scale=so, blocks=dev(lists), query_block=qb, x_layout=xl, y_layout=yl, m_tokens=m)
     torch.cuda.synchronize()
+    if path is not None:
+        assert hip.last_path() == "attention " + path
     got = y.cpu().numpy()
     got = hip.from_t16x32(got, m, nh * hd) if yl == T else got
     used = start[-1]
@@ -57,3 +59,47 @@ def test_lists(hip, qb):
         x = bars.codes(rng, sum(lens), 3 * nh * hd)
         for kind in (1, 3):
             check(hip, x, lens, nh, nh, hd, kind, key_len=keys, lists=lists, qb=qb)
+
+
+# lengths whose last 256, 32 and 64 tokens end everywhere, none shorter than nothing
+MANY = [1030, 1, 257, 64, 1099, 0, 255, 1024, 31, 300, 65, 512]
+
+
+@pytest.mark.parametrize("hd,padded", [(16, 32), (32, 32), (48, 64), (64, 64)])
+@pytest.mark.parametrize("nh,nkv,kind,xl,yl,masked", [(12, 12, 1, 0, 0, False), (12, 3, 3, T, T, True),
+                                                      (12, 12, 3, 0, T, True), (12, 4, 1, T, 0, True)])
+def test_two_tiles_a_wave(hip, hd, padded, nh, nkv, kind, xl, yl, masked):
+    """Many sequences of 1024 tokens and more, and of every other length among them."""
+    rng = np.random.default_rng([hd, nh, nkv, kind])
+    keys = [1030, 0, 200, 63, 1, 0, 255, 960, 17, 299, 64, 450] if masked else None
+    x = bars.codes(rng, sum(MANY) + 3, (nh + 2 * nkv) * hd)  # (the last tokens belong to no sequence)
+    check(hip, x, MANY, nh, nkv, hd, kind, xl, yl, key_len=keys, path=f"{padded},2,4,1")
+
+
+@pytest.mark.parametrize("hd,padded", [(32, 32), (64, 64)])
+def test_two_tiles_a_wave_where_scores_grow(hip, hd, padded):
+    """m moves again and again, in the short last chunk too."""
+    rng = np.random.default_rng(hd)
+    nh = 12
+    x = bars.codes(rng, sum(MANY), 3 * nh * hd)
+    grow = np.concatenate([np.linspace(0.02, 1.0, n) for n in MANY])[:, None]
+    cols = slice(nh * hd, 2 * nh * hd)
+    x[:, cols] = np.clip(np.rint(x[:, cols] * grow * 2), -127, 127).astype(np.int8)
+    for kind in (1, 3):
+        check(hip, x, MANY, nh, nh, hd, kind, x_scale=0.15, path=f"{padded},2,4,1")
+
+
+@pytest.mark.parametrize("lens,nh,hd,lists,path", [
+    ([40] * 3, 2, 64, 0, "64,1,4,1"), ([300], 2, 64, 0, "64,1,1,4"), ([300], 2, 128, 0, "128,1,1,4"),
+    ([1030] * 3, 8, 32, 0, "32,1,1,4"), ([300] * 30, 3, 96, 0, "96,1,4,1"), ([300] * 40, 4, 80, 0, "96,1,4,1"),
+    ([300], 2, 64, 64, "64,1,1,4 lists"), ([300] * 30, 4, 64, 16, "64,1,1,1 lists"),
+    ([300] * 30, 4, 64, 64, "64,1,2,1 lists"), ([300] * 30, 4, 64, 128, "64,1,4,1 lists"),
+    ([300] * 30, 4, 128, 32, "128,1,4,1 lists")])
+def test_other_shapes(hip, lens, nh, hd, lists, path):
+    rng = np.random.default_rng([len(lens), nh, hd])
+    x = bars.codes(rng, sum(lens), 3 * nh * hd)
+    rows = None
+    if lists:
+        rows = rng.permuted(np.tile(np.arange(6), (len(lens), nh, -(-max(lens) // lists), 1)), axis=-1)[..., :4]
+    for kind in (1, 3):
+        check(hip, x, lens, nh, nh, hd, kind, lists=rows, qb=lists or 64, path=path)
