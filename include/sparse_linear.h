@@ -303,7 +303,10 @@ sl_status residual_norm(const sl_residual_norm_args *args, void *hip_stream);
  *   kind        SL_EPI_F32 (y fp32, row-major) or SL_EPI_I8 (codes of out_scale
  *               in y_layout)
  *   y           [m_tokens x n_heads * head_dim], 16-byte aligned
- * Softmax weights enter the products with 22 bits.
+ * x_scale^2 * softmax_scale enters the exponentials with 22 bits. Softmax weights
+ * enter the products with 22 bits, but to no finer step than 2^-31 of the row's
+ * largest weight (2^-28 where x_scale^2 * softmax_scale is 0.92 or more, 2^-24
+ * from 7.39 on).
  * Errors: SL_ERR_INVALID_ARG, SL_ERR_SHAPE (sizes), SL_ERR_UNSUPPORTED (more
  * work items than a launch takes).
  */

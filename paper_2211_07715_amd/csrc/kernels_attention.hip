@@ -58,9 +58,9 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr int kChunk = SL_KEY_BLOCK;      // keys of a step
 constexpr int32_t kMagic = 0x4B400000;    // bits of 1.5 * 2^23
 constexpr float kMagicF = 12582912.0f;
-// P carries a factor 2^kFactor (small weights keep more of their bits). A lane's 32 weights of a chunk then sum to
-// 2^(kFactor + 5) at most where m is the maximum; while they sum to less than kMostSum, none is over what 16 bits hold.
-constexpr int kFactor = 7;
+// P carries a factor of up to 2^8 (see launch_attention), so that small weights keep more of their bits. A lane's 32
+// weights of a chunk then sum to 2^13 at most where m is the maximum; while they sum to less than kMostSum, none is over
+// what 16 bits hold.
 constexpr float kMostSum = 60000.0f;
 // m before the first key: below every score, and close enough that S - m keeps within the offset's 2^22
 constexpr int32_t kLowest = -(1 << 21);
@@ -413,6 +413,9 @@ void attention_kernel(const AttnArgs a)
         // the value cut to 11 bits, so the second is its remainder exactly: together
         // they hold 22, and a product with both costs matrix instructions, which
         // there is room for, where one of 11 bits changed 0.4 % of int8 results.
+        // The remainder of a weight below 2^-10 of the largest is a subnormal of 16
+        // bits: such weights are held to 2^-31 of the largest instead (the factor of
+        // 2^7 that P carries included). The sum is that of the whole values.
         f16x8 p[QT][4], p2[QT][4];
         const auto weights = [&](int t, const i32x16 (&s)[2]) __attribute__((always_inline)) {
             float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -875,9 +878,15 @@ sl_status launch_attention(const sl_attention_args &args, void *stream)
     int e = 0;
     const double frac = frexp(c2, &e);
     a.c2 = (float)ldexp(nearbyint(ldexp(frac, 22)), e - 22);
-    // (past 2^24 the offset takes no whole number: weights of neighbouring scores differ by a factor of 2.5 there)
-    const bool fits = kMagicF * a.c2 < 16777216.0f;
-    a.k2 = (fits ? (float)kFactor : 0.0f) - kMagicF * a.c2;
+    // P's factor is 2^7, and past 2^24 what the offset can take without losing a bit: multiples of 2, 4 and 8 up to 2^27,
+    // then nothing (weights of neighbouring scores differ by 10 octaves and more there, at 2^24 by 1.3)
+    const float offset = kMagicF * a.c2;
+    const float factor = offset < 0x1p24f   ? 7.0f
+                         : offset < 0x1p25f ? 6.0f
+                         : offset < 0x1p26f ? 4.0f
+                         : offset < 0x1p27f ? 8.0f
+                                            : 0.0f;
+    a.k2 = factor - offset;
     a.xs = args.x_scale;
     a.y_f32 = args.kind == SL_EPI_F32;
     a.inv_so = args.kind == SL_EPI_I8 ? 1.0f / args.out_scale : 1.0f;

@@ -103,3 +103,51 @@ def test_other_shapes(hip, lens, nh, hd, lists, path):
         rows = rng.permuted(np.tile(np.arange(6), (len(lens), nh, -(-max(lens) // lists), 1)), axis=-1)[..., :4]
     for kind in (1, 3):
         check(hip, x, lens, nh, nh, hd, kind, lists=rows, qb=lists or 64, path=path)
+
+
+def check_one_row(hip, n, hd, x, x_scale, sm, kind, step):
+    """A sequence whose queries are all alike: its one row of results."""
+    import torch
+    xs, scale = float(np.float32(x_scale)), float(np.float32(sm))
+    one = np.zeros((n, 3 * hd), np.int8)
+    one[:1, :hd] = x[:1, :hd]
+    one[:, hd:] = x[:, hd:]
+    q, k, v = one[0, :hd].astype(np.float64), one[:, hd:2 * hd].astype(np.float64), one[:, 2 * hd:] * xs
+    z = k @ q * (xs * xs * scale * np.log2(np.e))
+    w = np.exp2(z - z.max())
+    a = w @ np.abs(v) / w.sum()
+    rel = 2.0 ** -23 + (z.max() - z.min() + 16) * 2.0 ** -22 + 2.0 ** -21
+    bar = (2 * rel + (n / 4 + n / 64 + 32) * 2.0 ** -24) * a + step * np.abs(v).sum(0) / w.sum()
+    want = w @ v / w.sum()
+    so = bars.output_scale(want)
+    y = hip.attention(torch.from_numpy(x).cuda(), xs, torch.tensor([0, n], dtype=torch.int32, device="cuda"), n, 1, hd,
+                      softmax_scale=sm, kind=kind, out_scale=so).cpu().numpy()
+    for got in (y[0], y[n // 2], y[-1]):
+        bars.judge(got, want, bar, so if kind == 3 else None)
+    assert (y == y[0]).all()
+
+
+@pytest.mark.parametrize("kind", [1, 3])
+@pytest.mark.parametrize("n,hd", [(500, 64), (20000, 64), (20000, 32), (3000, 128)])
+def test_many_small_weights(hip, n, hd, kind):
+    """Keys of 2^-14 to 2^-18 of one key's weight, which has no value: the results are theirs alone."""
+    rng = np.random.default_rng([n, hd])
+    x = np.zeros((n, 3 * hd), np.int8)
+    x[:, 0], x[0, hd] = 100, 90
+    x[1:, hd] = rng.integers(0, 20, n - 1)
+    x[1:, 2 * hd:] = rng.integers(20, 120, (n - 1, hd))
+    check_one_row(hip, n, hd, x, 0.1, 18 / (9000 * 0.01 * np.log2(np.e)), kind, bars.STEP)
+
+
+@pytest.mark.parametrize("kind", [1, 3])
+@pytest.mark.parametrize("octaves", [0.5, 1.3, 1.34, 1.41, 1.9, 2.6, 2.7, 3.3, 4.9, 5.4, 6.1, 9.7, 10.6, 10.7, 14.3, 40.0])
+def test_small_weights_of_coarse_scores(hip, octaves, kind):
+    """Scales at which a step of the whole-number scores is worth that many octaves of weight."""
+    n, hd = 500, 64
+    rng = np.random.default_rng(5)
+    step = bars.STEP if octaves < 4 / 3 else 2.0 ** -28 if octaves < 32 / 3 else 2.0 ** -24
+    for far in (9.0, 10.5, 12.0, 13.5):
+        x = np.zeros((n, 3 * hd), np.int8)
+        x[:, 0], x[0, hd] = 1, max(1, round(far / octaves))
+        x[1:, 2 * hd:] = rng.integers(20, 120, (n - 1, hd))
+        check_one_row(hip, n, hd, x, 1.0, octaves / np.log2(np.e), kind, step)
