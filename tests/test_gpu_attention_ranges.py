@@ -1,0 +1,53 @@
+"""GPU tests of what attention_run and attention_select do with sizes at and past
+their ranges: starts and key lengths that are brought in, nothing to do, and launches
+of more work than one takes."""
+import numpy as np
+import pytest
+
+import attention_bars as bars
+import encoder_ref as ref
+
+pytestmark = pytest.mark.gpu
+T = 1  # LAYOUT_T16X32
+
+
+def _i32(values):
+    import torch
+    return torch.tensor(values, dtype=torch.int32, device="cuda")
+
+
+@pytest.mark.parametrize("kind", [1, 3])
+@pytest.mark.parametrize("layout", [0, T])
+@pytest.mark.parametrize("given,keys,inside,inside_keys", [
+    ([-5, 40, 1000], None, [0, 40, 150], None),
+    ([-(2 ** 31), 2, 2 ** 31 - 1], None, [0, 2, 150], None),
+    ([7, 90, 5000], [-3, 1000], [7, 90, 150], [0, 60]),
+    ([-1, 65, 150], [2 ** 31 - 1, -(2 ** 31)], [0, 65, 150], [65, 0]),
+    ([300, 400, 500], None, [150, 150, 150], None)])
+def test_starts_and_key_lengths_are_brought_in(hip, given, keys, inside, inside_keys, layout, kind):
+    """Every token of every sequence as with the numbers that they are brought to; tokens of none stay as they are."""
+    import torch
+    m, nh, hd = 150, 2, 64
+    x = bars.codes(np.random.default_rng(1), m, 3 * nh * hd)
+    xd = torch.from_numpy(np.ascontiguousarray(hip.to_t16x32(x, fill=99) if layout == T else x)).cuda()
+
+    def both(starts, key_len):
+        start, kl = _i32(starts), None if key_len is None else _i32(key_len)
+        args = dict(key_len=kl, x_layout=layout, m_tokens=m)
+        blocks = hip.select_blocks(xd, start, m, nh, hd, 2, **args)
+        out = []
+        for lists in (None, blocks):
+            y = torch.full((m, nh * hd), 77, dtype=torch.float32 if kind == 1 else torch.int8, device="cuda")
+            out.append(hip.attention(xd, 0.04, start, m, nh, hd, kind=kind, out_scale=0.02, blocks=lists, out=y, **args))
+        torch.cuda.synchronize()
+        return [t.cpu().numpy() for t in (blocks, *out)]
+
+    got, want = both(given, keys), both(inside, inside_keys)
+    for a, b in zip(got, want):
+        assert np.array_equal(a, b)
+    assert np.array_equal(got[0], ref.select(x, np.array(inside), nh, nh, hd, 2, m, 64, inside_keys))
+    y, bar = bars.attention(x, float(np.float32(0.04)), np.array(inside), nh, nh, hd, hd ** -0.5, inside_keys)
+    first, last = inside[0], inside[-1]
+    so = float(np.float32(0.02)) if kind == 3 else None
+    bars.judge(got[1][first:last], y[first:last], bar[first:last], so)
+    assert (got[1][:first] == 77).all() and (got[1][last:] == 77).all()
