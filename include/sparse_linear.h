@@ -346,7 +346,7 @@ sl_status attention_run(const sl_attention_args *args, void *hip_stream);
  *   workspace  attention_select_workspace(args) bytes, 16-byte aligned, held
  *              until the stream has passed the call
  * args: as for attention_run (blocks, y, kind, y_layout and the scales are not
- * read); max_len at most 262144 (SL_ERR_UNSUPPORTED), and no sequence longer
+ * read; m_tokens 0: no-op, no list is written); max_len at most 262144 (SL_ERR_UNSUPPORTED), and no sequence longer
  * than max_len (its blocks from there on are not considered).
  */
 int64_t attention_select_workspace(const sl_attention_args *args);

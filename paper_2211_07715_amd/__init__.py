@@ -531,6 +531,9 @@ def select_blocks(qkv, seq_start, max_len: int, n_heads: int, head_dim: int, top
         out = torch.empty(shape, dtype=torch.int32, device=qkv.device)
     elif out.dtype != torch.int32 or tuple(out.shape) != shape or not out.is_contiguous() or not out.is_cuda:
         raise ValueError(f"out must be a contiguous CUDA int32 tensor of shape {shape}")
+    if m == 0:  # (the call writes nothing)
+        with torch.cuda.stream(stream):  # (None: the current one)
+            return out.fill_(-1)
     args = _ATTN_ARGS.pack(qkv.data_ptr(), m, seq_start.data_ptr(), 0 if key_len is None else key_len.data_ptr(), 0, 0,
                            n_seq, max_len, x_layout, n_heads, n_kv, head_dim, top_k, query_block, EPI_F32, LAYOUT_ROWS,
                            1.0, 1.0, 1.0)

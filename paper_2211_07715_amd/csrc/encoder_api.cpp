@@ -155,9 +155,8 @@ sl_status attention_select(const sl_attention_args *args, int32_t *blocks, void 
     if (st == SL_OK) st = check_lists(a);
     if (st != SL_OK) return st;
     REFUSE_IF(a.max_len > 262144, SL_ERR_UNSUPPORTED, "max_len is over 262144");
-    if (a.n_seq == 0 || a.max_len == 0) return SL_OK;
+    if (a.m_tokens == 0 || a.n_seq == 0 || a.max_len == 0) return SL_OK;
     REFUSE_IF(!blocks || misaligned(blocks, 4), SL_ERR_INVALID_ARG, "blocks must be given and 4-byte aligned");
-    REFUSE_IF(a.m_tokens == 0, SL_ERR_SHAPE, "m_tokens is 0 with max_len over 0");
     REFUSE_IF(workspace_bytes < pooled_slots(a) * a.n_kv_heads * a.head_dim * 2, SL_ERR_INVALID_ARG,
               "workspace_bytes is below attention_select_workspace()");
     REFUSE_IF(!workspace || misaligned(workspace, 16), SL_ERR_INVALID_ARG,

@@ -16,6 +16,21 @@ def _i32(values):
     return torch.tensor(values, dtype=torch.int32, device="cuda")
 
 
+def test_no_tokens(hip):
+    """An empty batch of sequences is nothing to do with lists as without them; the lists name no block."""
+    import torch
+    for layout in (0, T):
+        x = torch.empty(hip.t16x32_shape(0, 192) if layout == T else (0, 192), dtype=torch.int8, device="cuda")
+        args = dict(x_layout=layout, m_tokens=0)
+        out = torch.full((3, 1, 2, 4), 5, dtype=torch.int32, device="cuda")
+        for blocks in (hip.select_blocks(x, _i32([0, 0, 0, 0]), 128, 1, 64, 4, **args),
+                       hip.select_blocks(x, _i32([0, 0, 0, 0]), 128, 1, 64, 4, out=out, stream=torch.cuda.Stream(), **args)):
+            torch.cuda.synchronize()
+            assert blocks.shape == (3, 1, 2, 4) and (blocks == -1).all()
+            y = hip.attention(x, 0.04, _i32([0, 0, 0, 0]), 128, 1, 64, kind=1, blocks=blocks, **args)
+            assert y.shape == (0, 64)
+
+
 @pytest.mark.parametrize("kind", [1, 3])
 @pytest.mark.parametrize("layout", [0, T])
 @pytest.mark.parametrize("given,keys,inside,inside_keys", [
