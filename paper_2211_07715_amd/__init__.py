@@ -453,6 +453,8 @@ def _attention_args(x, seq_start, max_len, n_heads, head_dim, n_kv_heads, key_le
     """Checks of what attention and select_blocks share; returns (m_tokens, n_kv_heads, n_seq)."""
     torch = _torch or _torch_once()
     n_kv = n_heads if n_kv_heads is None else n_kv_heads
+    if head_dim < 1:
+        raise ValueError("head_dim must be >= 1")
     cols = (n_heads + 2 * n_kv) * head_dim
     if x.dtype != torch.int8 or not x.is_cuda or not x.is_contiguous():
         raise ValueError("qkv must be a contiguous CUDA int8 tensor")
@@ -500,6 +502,8 @@ def attention(qkv, x_scale: float, seq_start, max_len: int, n_heads: int, head_d
         raise ValueError("out has the wrong dtype/shape or is not contiguous")
     lists, top_k = 0, 0
     if blocks is not None:
+        if query_block < 1:
+            raise ValueError("query_block must be >= 1")
         want = (n_seq, n_heads, -(-max_len // query_block))
         if blocks.dtype != torch.int32 or not blocks.is_cuda or not blocks.is_contiguous() or blocks.dim() != 4 or \
                 tuple(blocks.shape[:3]) != want:
@@ -524,8 +528,8 @@ def select_blocks(qkv, seq_start, max_len: int, n_heads: int, head_dim: int, top
     m, n_kv, n_seq = _attention_args(qkv, seq_start, max_len, n_heads, head_dim, n_kv_heads, key_len, x_layout,
                                      m_tokens)
     torch = _torch
-    if query_block < 1 or top_k < 1:
-        raise ValueError("query_block and top_k must be >= 1")
+    if query_block < 1 or top_k < 1 or n_heads < 0 or max_len < 0:
+        raise ValueError("query_block and top_k must be >= 1, n_heads and max_len >= 0")
     shape = (n_seq, n_heads, -(-max_len // query_block), top_k)
     if out is None:
         out = torch.empty(shape, dtype=torch.int32, device=qkv.device)

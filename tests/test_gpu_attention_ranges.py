@@ -16,6 +16,32 @@ def _i32(values):
     return torch.tensor(values, dtype=torch.int32, device="cuda")
 
 
+def test_sizes_that_are_none(hip):
+    """Refused by name: by the binding where it makes a shape or a scale of them, otherwise by the library."""
+    import torch
+    x = torch.zeros((64, 3 * 64), dtype=torch.int8, device="cuda")
+    start = _i32([0, 64])
+    lists = torch.zeros((1, 1, 1, 1), dtype=torch.int32, device="cuda")
+    for qb in (0, -64):
+        with pytest.raises(ValueError):
+            hip.attention(x, 0.04, start, 64, 1, 64, kind=1, blocks=lists, query_block=qb)
+        with pytest.raises(ValueError):
+            hip.select_blocks(x, start, 64, 1, 64, 1, query_block=qb)
+    none = torch.zeros((64, 0), dtype=torch.int8, device="cuda")
+    for nh, hd, nkv, t, error in ((1, 0, 1, none, ValueError), (-1, -64, -1, x, ValueError), (1, -64, -2, x, ValueError),
+                                  (0, 64, 0, none, hip.SparseLinearError), (3, 64, 0, x, hip.SparseLinearError)):
+        with pytest.raises(error):
+            hip.attention(t, 0.04, start, 64, nh, hd, n_kv_heads=nkv, kind=1)
+        with pytest.raises(error):
+            hip.select_blocks(t, start, 64, nh, hd, 1, n_kv_heads=nkv)
+    with pytest.raises(ValueError):
+        hip.select_blocks(x, start, -64, 1, 64, 1)
+    with pytest.raises(ValueError):
+        hip.attention(x, 0.04, start, -64, 1, 64, blocks=lists)
+    with pytest.raises(hip.SparseLinearError):
+        hip.attention(x, 0.04, start, -64, 1, 64)
+
+
 def test_no_tokens(hip):
     """An empty batch of sequences is nothing to do with lists as without them; the lists name no block."""
     import torch
