@@ -711,6 +711,7 @@ struct SelectArgs {
     int32_t *blocks;
     int64_t m, slots;
     int32_t n_seq, n_heads, n_kv, hd, cols, x_cb, top_k, qb, n_qb, max_blocks;
+    int32_t seq0, head0;  // first of this launch
 };
 
 // Pooled keys: one wave a key block and 64 features of the keys, 4 features a
@@ -718,7 +719,7 @@ struct SelectArgs {
 // tokens of 12 heads of 64: 5.1 us, 2.5 TB/s).
 __global__ __launch_bounds__(256) void pool_keys_kernel(const SelectArgs a)
 {
-    const int32_t seq = blockIdx.z, b = blockIdx.y, lane = threadIdx.x & 63;
+    const int32_t seq = a.seq0 + blockIdx.z, b = blockIdx.y, lane = threadIdx.x & 63;
     const Span sp = span_of(a.seq_start, a.key_len, seq, a.m);
     const int32_t have = min(sp.keys - b * kChunk, kChunk);
     const int32_t c = (blockIdx.x * 4 + threadIdx.x / 64) * 64 + lane % 16 * 4;  // of the key columns
@@ -763,7 +764,7 @@ __global__ __launch_bounds__(64) void select_blocks_kernel(const SelectArgs a)
     __shared__ int32_t qsum[128];
     __shared__ __attribute__((aligned(16))) int16_t q16[128];
     const int lane = threadIdx.x;
-    const int32_t qb = blockIdx.x, head = blockIdx.y, seq = blockIdx.z;
+    const int32_t qb = blockIdx.x, head = a.head0 + blockIdx.y, seq = a.seq0 + blockIdx.z;
     const Span sp = span_of(a.seq_start, a.key_len, seq, a.m);
     int32_t *list = a.blocks + (((int64_t)seq * a.n_heads + head) * a.n_qb + qb) * a.top_k;
     const int32_t rows_n = min(sp.n - qb * a.qb, a.qb);
@@ -919,23 +920,27 @@ sl_status launch_attention_select(const sl_attention_args &args, int32_t *blocks
     a.qb = args.query_block;
     a.n_qb = (args.max_len + a.qb - 1) / a.qb;
     a.max_blocks = (args.max_len + kChunk - 1) / kChunk;
-    if (a.n_seq > 65535 || a.n_heads > 65535) {
-        set_error("more than 65535 sequences or heads");
-        return SL_ERR_UNSUPPORTED;
-    }
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    hipLaunchKernelGGL(pool_keys_kernel, dim3((a.n_kv * a.hd + 255) / 256, a.max_blocks, a.n_seq), dim3(256), 0, s, a);
-    HIP_TRY(hipGetLastError());
-    const dim3 grid(a.n_qb, a.n_heads, a.n_seq);
-    if (a.max_blocks <= 64)
-        hipLaunchKernelGGL(select_blocks_kernel<1>, grid, dim3(64), 0, s, a);
-    else if (a.max_blocks <= 256)
-        hipLaunchKernelGGL(select_blocks_kernel<4>, grid, dim3(64), 0, s, a);
-    else if (a.max_blocks <= 1024)
-        hipLaunchKernelGGL(select_blocks_kernel<16>, grid, dim3(64), 0, s, a);
-    else
-        hipLaunchKernelGGL(select_blocks_kernel<64>, grid, dim3(64), 0, s, a);
-    HIP_TRY(hipGetLastError());
+    constexpr int32_t kMostGrid = 65535;  // workgroups of a launch in its second and third dimension
+    for (int64_t s0 = 0; s0 < a.n_seq; s0 += kMostGrid) {
+        a.seq0 = (int32_t)s0;
+        const int32_t seqs = std::min(a.n_seq - a.seq0, kMostGrid);
+        hipLaunchKernelGGL(pool_keys_kernel, dim3((a.n_kv * a.hd + 255) / 256, a.max_blocks, seqs), dim3(256), 0, s, a);
+        HIP_TRY(hipGetLastError());
+        for (int32_t h0 = 0; h0 < a.n_heads; h0 += kMostGrid) {
+            a.head0 = h0;
+            const dim3 grid(a.n_qb, std::min(a.n_heads - h0, kMostGrid), seqs);
+            if (a.max_blocks <= 64)
+                hipLaunchKernelGGL(select_blocks_kernel<1>, grid, dim3(64), 0, s, a);
+            else if (a.max_blocks <= 256)
+                hipLaunchKernelGGL(select_blocks_kernel<4>, grid, dim3(64), 0, s, a);
+            else if (a.max_blocks <= 1024)
+                hipLaunchKernelGGL(select_blocks_kernel<16>, grid, dim3(64), 0, s, a);
+            else
+                hipLaunchKernelGGL(select_blocks_kernel<64>, grid, dim3(64), 0, s, a);
+            HIP_TRY(hipGetLastError());
+        }
+    }
     return SL_OK;
 }
 

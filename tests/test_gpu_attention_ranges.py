@@ -92,3 +92,50 @@ def test_starts_and_key_lengths_are_brought_in(hip, given, keys, inside, inside_
     so = float(np.float32(0.02)) if kind == 3 else None
     bars.judge(got[1][first:last], y[first:last], bar[first:last], so)
     assert (got[1][:first] == 77).all() and (got[1][last:] == 77).all()
+
+
+def _select(hip, x, start, nh, nkv, hd, top_k, max_len, qb):
+    import torch
+    print(f"select {len(start) - 1} sequences to {max_len}, heads {nh}/{nkv}x{hd}, query_block {qb}", flush=True)
+    out = hip.select_blocks(torch.from_numpy(x).cuda(), _i32(start.tolist()), max_len, nh, hd, top_k, n_kv_heads=nkv,
+                            query_block=qb)
+    torch.cuda.synchronize()
+    return out
+
+
+def test_select_of_many_sequences(hip):
+    """More sequences than a launch has a dimension for."""
+    rng = np.random.default_rng(3)
+    lens = np.minimum(rng.geometric(0.6, 70000) - 1, 5)
+    lens[[5, 65535, 65536, 69999]] = 150, 140, 200, 131
+    x = bars.codes(rng, int(lens.sum()), 3 * 16)
+    start = bars.starts(lens)
+    got = _select(hip, x, start, 1, 1, 16, 2, 200, 64).cpu().numpy()
+    assert np.array_equal(got, ref.select(x, start, 1, 1, 16, 2, 200, 64))
+
+
+def test_select_of_many_heads(hip):
+    rng = np.random.default_rng(4)
+    lens, nh = [40, 150], 66000
+    x = bars.codes(rng, sum(lens), (nh + 4) * 16)
+    start = bars.starts(lens)
+    got = _select(hip, x, start, nh, 2, 16, 2, 150, 64).cpu().numpy()
+    assert np.array_equal(got, ref.select(x, start, nh, 2, 16, 2, 150, 64))
+
+
+@pytest.mark.parametrize("nh,n_seq,max_len,qb", [(1024, 66, 8192, 16), (1, 2100, 262144, 128), (2048, 66, 8192, 16)])
+def test_select_of_more_than_a_launch(hip, nh, n_seq, max_len, qb):
+    """Lists, or blocks of keys, of 2^31 and 2^32 threads and more; nearly all of sequences much shorter than max_len."""
+    import torch
+    rng = np.random.default_rng(n_seq)
+    lens = [1] * n_seq
+    lens[0], lens[7], lens[-1] = 150, 200, 131
+    x = bars.codes(rng, sum(lens), (nh + 2) * 16)
+    start = bars.starts(lens)
+    got = _select(hip, x, start, nh, 1, 16, 1, max_len, qb)
+    for s in (0, 1, 7, n_seq - 2, n_seq - 1):
+        want = ref.select(x[start[s]:start[s + 1]], np.array([0, lens[s]]), nh, 1, 16, 1, max(lens), qb)[0]
+        assert np.array_equal(got[s, :, :want.shape[1]].cpu().numpy(), want)
+        got[s, :, :want.shape[1]] = -1
+    got[:, :, 0] = torch.where(got[:, :, 0] == 0, -1, got[:, :, 0])  # (a sequence of one token has its one block)
+    assert bool((got == -1).all())
