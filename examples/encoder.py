@@ -87,7 +87,8 @@ class Encoder:
         return torch.cat(out)
 
     def __call__(self, x, start, longest, top_k=0, tap=None):
-        """x: fp32 [tokens, hidden]; start: int32 sequence starts on the device. tap(name, tensor) sees every result."""
+        """x: fp32 [tokens, hidden]; start: int32 sequence starts on the device. tap(i, results) sees
+        what layer i left on the device, by name."""
         m, d, s = x.shape[0], self.hidden // self.heads, self.scales
         tap = tap or (lambda *a: None)
         blocks = dict(x_layout=BLOCKS, m_tokens=m)
