@@ -302,7 +302,7 @@ sl_status residual_norm(const sl_residual_norm_args *args, void *hip_stream);
  *   query_block 16, 32, 64 or 128; top_k >= 1 (read only with `blocks`)
  *   kind        SL_EPI_F32 (y fp32, row-major) or SL_EPI_I8 (codes of out_scale
  *               in y_layout)
- *   y           [m_tokens x n_heads * head_dim], 16-byte aligned
+ *   y           [m_tokens x n_heads * head_dim], 16-byte aligned; overlaps no input
  * x_scale^2 * softmax_scale enters the exponentials with 22 bits. Softmax weights
  * enter the products with 22 bits, but to no finer step than 2^-31 of the row's
  * largest weight (2^-28 where x_scale^2 * softmax_scale is 0.92 or more, 2^-24

@@ -19,18 +19,22 @@
 // gives the exponent.
 //
 // What bounds it: the vector instructions (an exponential 8.3 cycles of a SIMD,
-// a conversion, permute or dot product 4.3, a fused multiply-add 2.6), with the
-// matrix instructions beside them. 32 x 32 ones take less of the issue than
-// 16 x 16 ones of the same work. m may lag behind the running maximum by a
-// factor of 2^8, which 16-bit P leaves room for: it moves, and l and O are
-// rescaled, outside the loop over chunks, which is left for that and entered
-// again (a branch inside would make the compiler copy every accumulator).
+// a conversion, permute or dot product 4.3, a fused multiply-add 2.6) with one
+// tile of queries a wave; with two, which stage a chunk half as often, vector and
+// matrix instructions together, which overlap only in part. 32 x 32 matrix ones
+// take less of the issue than 16 x 16 ones of the same work. m may lag behind the
+// running maximum by a factor of 2^8, which 16-bit P leaves room for: it moves,
+// and l and O are rescaled, outside the loop over chunks, which is left for that
+// and entered again (a branch inside would make the compiler copy every
+// accumulator).
 //
-// Measured, 4 operations a score and feature: 128 x 384 tokens of 12 heads of 64
-// 110 us (527 TOP/s; vector instructions issue 86 % of the time, matrix ones run
-// 35 %), 8192 tokens of 16 heads on 4 374 us (735 TOP/s; 76 %, 42 %), 32 blocks
-// at 16384 tokens of 12 heads 179 us (576 TOP/s; 77 %, 36 %), 32 x 128 tokens 8.6
-// us, 128 tokens 6.4 us.
+// Measured, 4 operations a score and feature, replayed from a graph: 128 x 384
+// tokens of 12 heads of 64 111 us (522 TOP/s), 8192 tokens of 16 heads on 4 367 us
+// (749 TOP/s), 32 blocks at 16384 tokens of 12 heads 171 us (603 TOP/s), 32 x 128
+// tokens 9.0 us, 128 tokens 6.5 us. In traced launches of the same three long
+// cases (110, 431 and 187 us) vector instructions are active up to 86, 73 and 77
+// % of the time (counted in steps of 4 cycles, more than a plain one takes),
+// and matrix ones run 35, 43 and 36 %.
 #include <hip/hip_runtime.h>
 #include <math.h>
 

@@ -12,9 +12,10 @@
 // int8 rows in either layout in 4-byte ones. W = 1 (up to 1024 features of many
 // rows) needs no barrier and no LDS.
 //
-// Measured: 4096 x 768, fp32 in and int8 out, 8.5 us (4.8 TB/s, of 5.1 that a
-// copy of 1 GiB reaches); 49152 x 1024, int8 y, norms on both sides, h kept, 117
-// us (4.3 TB/s); 1531 x 1001, fp32, 8.3 us (3.1 TB/s); 128 x 768 3.0 us.
+// Measured, replayed from a graph: 4096 x 768, fp32 in and int8 out, 8.4 us (4.9
+// TB/s, of 5.1 that a copy of 1 GiB reaches); 49152 x 1024, int8 y, norms on both
+// sides, h kept, 119 us (4.2 TB/s); 1531 x 1001, fp32, 8.1 us (3.2 TB/s); 128 x 768
+// 3.2 us; 49152 x 768, codes to codes, all in pieces of 4 bytes, 40 us (2.8 TB/s).
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -319,15 +320,15 @@ sl_status launch_residual_norm(const sl_residual_norm_args &a, void *stream)
     p.inv_so = a.q ? 1.0f / a.out_scale : 1.0f;
     if (a.cols <= 256) return launch_shape<1, 1, 4>(p, s);
     if (a.cols <= 512) return launch_shape<1, 2, 4>(p, s);
-    // Few rows: a row's chain of loads, sums and stores counts, and four waves shorten it. Up to 2048 rows: 128 x 768 3.0
-    // us against 3.9, 1024 x 1024 4.0 against 5.2, 1531 x 1001 with norms on both sides 8.3 against 10.5; 2048 x 768 5.8
-    // against 5.9. More: 49152 x 1024 126 against 121, with norms on both sides and int8 y 146 against 120.
+    // Few rows: a row's chain of loads, sums and stores counts, and four waves shorten it. Up to 2048 rows: 128 x 768 3.2
+    // us against 4.0, 1024 x 1024 4.5 against 4.8, 1531 x 1001 with norms on both sides 8.1 against 10.3; 2048 x 768 6.0
+    // against 5.8. More: 49152 x 1024 95 against 90, with norms on both sides, int8 y and h kept 146 against 118.
     if (a.rows <= 2048 && a.cols <= 1024) return launch_shape<4, 1, 4>(p, s);
     if (a.cols <= 768) return launch_shape<1, 3, 4>(p, s);
     if (a.cols <= 1024) return launch_shape<1, 4, 4>(p, s);
     if (a.cols <= 2048) return launch_shape<4, 2, 4>(p, s);
-    // (8192 x 2894 with four pieces a lane 77 us against 67; 8192 x 4096 on four waves 79 against 78, with norms on both
-    // sides 91 against 81)
+    // (8192 x 2894 with four pieces a lane 77 us against 66; 8192 x 4096 on four waves 79 against 77, with norms on both
+    // sides and a gate 100 against 90)
     if (a.cols <= 3072) return launch_shape<4, 3, 4>(p, s);
     if (a.cols <= 4096) return launch_shape<8, 2, 8>(p, s);
     if (a.cols <= 16384) return launch_shape<16, 4, 16>(p, s);
