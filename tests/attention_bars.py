@@ -62,7 +62,7 @@ def output_scale(want):
     return float(np.float32(max(np.abs(want).max(initial=0.0), 1e-3) / 126))
 
 
-def judge(got, want, bar, out_scale=None):
+def assert_within(got, want, bar, out_scale=None):
     """Asserts that fp32 results, or int8 codes of out_scale, are within the bars."""
     if got.size == 0:
         return

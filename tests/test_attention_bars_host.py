@@ -38,14 +38,14 @@ def test_a_lost_second_part_is_seen(lens, nh, hd):
     want, bar = run(lens, nh, hd, lambda w: w)
     so = bars.output_scale(want)
     for good in (want, run(lens, nh, hd, two_parts)[0]):
-        bars.judge(good.astype(np.float32), want, bar)
-        bars.judge(np.rint(good / so), want, bar, so)
+        bars.assert_within(good.astype(np.float32), want, bar)
+        bars.assert_within(np.rint(good / so), want, bar, so)
     bad = run(lens, nh, hd, one_part)[0]
     with pytest.raises(AssertionError):
-        bars.judge(np.rint(bad / so), want, bar, so)
+        bars.assert_within(np.rint(bad / so), want, bar, so)
     with pytest.raises(AssertionError):
-        bars.judge(bad.astype(np.float32), want, bar)
+        bars.assert_within(bad.astype(np.float32), want, bar)
     with pytest.raises(AssertionError):
-        bars.judge(np.trunc(want / so), want, bar, so)
+        bars.assert_within(np.trunc(want / so), want, bar, so)
     # (a bar of half a step and 2^-10 of the largest value, as for one part, would not have seen it)
     assert np.abs(np.rint(bad / so) - want / so).max() <= 0.5 + 2 * 2.0 ** -10 * 128 * 0.04 / so

@@ -29,7 +29,7 @@ def check(hip, x, lens, nh, nkv, hd, kind, xl=0, yl=0, x_scale=0.04, sm=None, ke
     got = y.cpu().numpy()
     got = hip.from_t16x32(got, m, nh * hd) if yl == T else got
     used = start[-1]
-    bars.judge(got[:used], want[:used], bar[:used], so if kind == 3 else None)
+    bars.assert_within(got[:used], want[:used], bar[:used], so if kind == 3 else None)
     return got
 
 
@@ -123,7 +123,7 @@ def check_one_row(hip, n, hd, x, x_scale, sm, kind, step):
     y = hip.attention(torch.from_numpy(x).cuda(), xs, torch.tensor([0, n], dtype=torch.int32, device="cuda"), n, 1, hd,
                       softmax_scale=sm, kind=kind, out_scale=so).cpu().numpy()
     for got in (y[0], y[n // 2], y[-1]):
-        bars.judge(got, want, bar, so if kind == 3 else None)
+        bars.assert_within(got, want, bar, so if kind == 3 else None)
     assert (y == y[0]).all()
 
 
