@@ -17,7 +17,7 @@ case is a dict of plain values; ``op`` says what one pass is:
 (``ragged``: numbers of both drawn from 1 on, one sequence idle: nothing cached);
 without ``causal`` the two are apart. Pages of ``ps`` tokens lie in any order. A
 page holds, for each key-value head, its keys [ps][hd] and then, for each, its
-values [ps / 4][hd][4]: four tokens' values of a feature lie together. ``layout``
+values [ps / 16][hd][16]: 16 tokens' values of a feature lie together. ``layout``
 is that of the int8 activations: ``rows`` or ``tiles`` (16 tokens x 32 features).
 Int8 results, the cache among them, are returned as the values they stand for, in
 bfloat16.
@@ -271,8 +271,8 @@ def _plain_append(s):
     page = s["table"][seq, at // ps].long()
     page, at, k, v = page[put], at[put] % ps, k[put], v[put]
     s["cache"][:, 0].index_put_((page[:, None], torch.arange(nkv, device=x.device)[None, :], at[:, None]), k)
-    values = s["cache"][:, 1].view(-1, nkv, ps // 4, hd, 4)
-    values[page, :, at // 4, :, at % 4] = v
+    values = s["cache"][:, 1].view(-1, nkv, ps // 16, hd, 16)
+    values[page, :, at // 16, :, at % 16] = v
     q = _codes(qk[:, :nh], s["q_scale"]).reshape(m, nh * hd).to(torch.bfloat16) * s["q_value"]
     return {"q": _tiles(q) if _whole(c, m) else q, "cache": s["cache"] * s["kv_value"]}
 
@@ -287,7 +287,7 @@ def _plain_attend(s):
     q = q.reshape(b, n, nkv, g, hd).permute(0, 2, 3, 1, 4).reshape(b, nkv, g * n, hd)
     pages = s["cache"][s["table"].long().clamp(min=0)]  # [b, per, 2, nkv, ps, hd]
     k = pages[:, :, 0].permute(0, 2, 4, 1, 3).reshape(b, nkv, hd, per * ps).float()
-    v = pages[:, :, 1].reshape(b, per, nkv, ps // 4, hd, 4).permute(0, 2, 1, 3, 5, 4)
+    v = pages[:, :, 1].reshape(b, per, nkv, ps // 16, hd, 16).permute(0, 2, 1, 3, 5, 4)
     v = v.reshape(b, nkv, per * ps, hd).float()
     p = (q @ k).mul_(s["q_scale"] * s["k_scale"] / math.sqrt(hd)).reshape(b, nkv, g, n, per * ps)
     last = s["len"].long()[:, None].expand(b, n)  # keys that a query sees
@@ -339,8 +339,8 @@ def exact(case, seed):
         place = torch.arange(t, device=q.device)
         for h in range(nkv):
             keys = s["cache"][page, 0, h].reshape(-1, hd)[:t].double() * s["k_scale"]
-            quads = s["cache"][page, 1, h].reshape(-1, hd, 4)
-            values = quads[place // 4, :, place % 4].double() * s["v_scale"]
+            groups = s["cache"][page, 1, h].reshape(-1, hd, 16)
+            values = groups[place // 16, :, place % 16].double() * s["v_scale"]
             for a in range(h * (nh // nkv), (h + 1) * (nh // nkv)):
                 z = (q[rows, a] @ keys.t()) / math.sqrt(hd)
                 if case["causal"]:
@@ -381,9 +381,9 @@ def _exact_append(case, s, news, lens, pages):
             continue
         for h in range(nkv):
             store[page[place // ps], 0, h, place % ps] = rounded(part[:, nh + h], s["k_scale"])
-            quads = store[:, 1, h].reshape(-1, ps // 4, hd, 4)  # (a copy)
-            quads[page[place // ps], place % ps // 4, :, place % 4] = rounded(part[:, nh + nkv + h], s["v_scale"])
-            store[:, 1, h] = quads.reshape(-1, ps, hd)
+            groups = store[:, 1, h].reshape(-1, ps // 16, hd, 16)  # (a copy)
+            groups[page[place // ps], place % ps // 16, :, place % 16] = rounded(part[:, nh + nkv + h], s["v_scale"])
+            store[:, 1, h] = groups.reshape(-1, ps, hd)
     q = q.reshape(m, nh * hd) * s["q_scale"]
     store[:, 0] *= s["k_scale"]
     store[:, 1] *= s["v_scale"]
