@@ -353,6 +353,155 @@ int64_t attention_select_workspace(const sl_attention_args *args);
 sl_status attention_select(const sl_attention_args *args, int32_t *blocks, void *workspace, int64_t workspace_bytes,
                            void *hip_stream);
 
+/*
+ * Keys and values of a decoder's tokens (or of an encoder's states that a
+ * decoder attends to) between its steps, as int8 codes in pages of page_size
+ * tokens. The cache is n_pages pages, each of 2 * n_kv_heads * page_size *
+ * head_dim bytes: for every key/value head its keys [page_size][head_dim], then
+ * for every head its values [page_size / 16][head_dim][16] (16 tokens' codes of a
+ * feature lie together: what a lane of the int8 matrix instructions takes).
+ * Slot p of sequence s lies in page page_table[s][p / page_size], place
+ * p % page_size; entries outside 0 .. n_pages - 1 (such as -1) name no page.
+ * Sequences may share pages that they only read. As in attention_run, a call's
+ * tokens lie one sequence after the other, s having n_s = seq_start[s+1] -
+ * seq_start[s] (seq_start is brought into 0 .. m_tokens); kv_len[s] counts its
+ * cached tokens with the call's own (below 0: 0), so its token i has slot
+ * kv_len[s] - n_s + i.
+ */
+typedef enum {
+    SL_ROPE_NONE = 0,
+    SL_ROPE_HALF = 1,       /* pairs of features (j, j + rope_dim / 2) */
+    SL_ROPE_INTERLEAVED = 2 /* pairs of features (2 j, 2 j + 1)        */
+} sl_rope_kind;
+
+/*
+ * What lies between a QKV linear of a decoder and cache_attention: rotates the
+ * queries and keys by position, writes the queries' codes, and the keys' and
+ * values' codes to the cache. With w = position * inv_freq[j] (in 64 bits), for a
+ * pair (a, b) of the first rope_dim features of every query and key head:
+ *   a' = rope_factor * (a cos w - b sin w),  b' = rope_factor * (b cos w + a sin w)
+ * and codes = clamp(rint(value * (1 / scale)), -127, 127) of q_scale, k_scale and
+ * v_scale. (With SL_ACT_I8, SL_ROPE_NONE and equal scales codes are copied.)
+ *   x           [m_tokens x (n_heads + 2 n_kv_heads) * head_dim] fp32 row-major
+ *               (SL_ACT_F32; finite) or int8 codes of x_scale in x_layout
+ *               (SL_ACT_I8): all query heads, then key heads, then value heads;
+ *               16-byte aligned
+ *   positions   [m_tokens] int32 device, or NULL: a token's slot
+ *   inv_freq    [rope_dim / 2] fp32 device (read unless SL_ROPE_NONE)
+ *   cache       16-byte aligned. Tokens whose slot is below 0, from max_pages *
+ *               page_size on, or in no page are not stored; two tokens of one slot
+ *               leave an unspecified mix of both.
+ *   q           [m_tokens x n_heads * head_dim] int8 in q_layout, 16-byte aligned,
+ *               or NULL: not written. Padding and tokens of no sequence are left
+ *               as they are.
+ *   max_new     largest n_s: what the launch is sized by (longer sequences are
+ *               still done whole; 0: no-op)
+ *   max_pages   entries of page_table a sequence, max_pages * page_size at most
+ *               2^31 - 65536
+ *   page_size   16, 32, 64, 128 or 256
+ *   n_heads     a multiple of n_kv_heads, or 0: x holds keys and values only
+ *   rope_dim    even, 2 .. head_dim; inv_freq slower and rope_factor other than 1
+ *               serve contexts scaled beyond the trained ones
+ * cache and q overlap no input. Allocates nothing, never synchronises.
+ * Errors: SL_ERR_INVALID_ARG, SL_ERR_SHAPE (sizes), SL_ERR_UNSUPPORTED (more
+ * work items than a launch takes).
+ */
+typedef struct {
+    const void *x;
+    int64_t m_tokens;
+    const int32_t *seq_start;
+    const int32_t *kv_len;
+    const int32_t *page_table;
+    const int32_t *positions;
+    const float *inv_freq;
+    int8_t *cache;
+    int8_t *q;
+    int32_t n_seq;
+    int32_t max_new;
+    int32_t max_pages;
+    int32_t n_pages;
+    int32_t page_size;
+    int32_t x_type;
+    int32_t x_layout;
+    int32_t n_heads;
+    int32_t n_kv_heads;
+    int32_t head_dim;
+    int32_t rope_kind;
+    int32_t rope_dim;
+    int32_t q_layout;
+    float x_scale;
+    float rope_factor;
+    float q_scale;
+    float k_scale;
+    float v_scale;
+} sl_cache_append_args;
+
+sl_status cache_append(const sl_cache_append_args *args, void *hip_stream);
+
+/*
+ * Attention of a call's tokens over what their sequences have cached: one new
+ * token a sequence, several, or whole prompts; with `causal` token i sees the
+ * slots up to its own, without it all kv_len[s] (cross attention to states of
+ * another length, whose number then has nothing to do with n_s). For query head
+ * a, with key/value head a / (n_heads / n_kv_heads) and the exact integers q.k:
+ *   z_j = q_scale * k_scale * softmax_scale * (q . k_j)
+ *   y   = v_scale * sum_j softmax(z)_j v_j
+ * over the slots seen that lie in a page of the table (none: y = 0).
+ *   q           [m_tokens x q_cols] int8 codes in q_layout, 16-byte aligned, whose
+ *               first n_heads * head_dim features are the queries (cache_append's
+ *               q; without rotation also a QKV linear's own output)
+ *   q_cols      >= n_heads * head_dim, row-major a multiple of 16, at most 2^24
+ *   max_new     largest n_s, as in cache_append
+ *   max_len     largest kv_len: with max_new what the launch is sized by (longer
+ *               ones are still computed whole)
+ *   causal      0 or 1
+ *   kind        SL_EPI_F32 (y fp32, row-major) or SL_EPI_I8 (codes of out_scale in
+ *               y_layout)
+ *   y           [m_tokens x n_heads * head_dim], 16-byte aligned; overlaps no
+ *               input. Tokens of no sequence are not written.
+ *   workspace   cache_attention_workspace(args) bytes (0: may be NULL), 16-byte
+ *               aligned, held until the stream has passed the call; calls that may
+ *               run at the same time each have their own
+ * Other fields as in cache_append. Softmax weights enter the products as 23-bit
+ * parts of a span's largest (spans of up to 128 keys), or, for many queries, as
+ * in attention_run. Results do not depend on timing.
+ * Errors: SL_ERR_INVALID_ARG, SL_ERR_SHAPE (sizes), SL_ERR_UNSUPPORTED (more
+ * work items than a launch takes).
+ */
+typedef struct {
+    const int8_t *q;
+    int64_t m_tokens;
+    const int32_t *seq_start;
+    const int32_t *kv_len;
+    const int32_t *page_table;
+    const int8_t *cache;
+    void *y;
+    void *workspace;
+    int64_t workspace_bytes;
+    int32_t n_seq;
+    int32_t max_new;
+    int32_t max_len;
+    int32_t max_pages;
+    int32_t n_pages;
+    int32_t page_size;
+    int32_t q_layout;
+    int32_t q_cols;
+    int32_t n_heads;
+    int32_t n_kv_heads;
+    int32_t head_dim;
+    int32_t causal;
+    int32_t kind;
+    int32_t y_layout;
+    float q_scale;
+    float k_scale;
+    float v_scale;
+    float softmax_scale;
+    float out_scale;
+} sl_cache_attention_args;
+
+int64_t cache_attention_workspace(const sl_cache_attention_args *args);
+sl_status cache_attention(const sl_cache_attention_args *args, void *hip_stream);
+
 /* Rebuild the dense [n_out x k_in] int8 weight from the handle's GPU tile
  * image (host mirror), into caller memory w_host. Round trip of the packer. */
 sl_status sparse_linear_unpack(const sl_packed_weight *w, int8_t *w_host);

@@ -25,6 +25,15 @@ in the token dimension, seq_start their first tokens and the end):
     blocks = sl.select_blocks(qkv, seq_start, max_len, n_heads, head_dim, top_k)            # long sequences:
     a = sl.attention(qkv, s_qkv, seq_start, max_len, n_heads, head_dim, out_scale=s_a, blocks=blocks)
     _, u, q = sl.residual_norm(y, gamma, beta, residual=x, keep_norm=True, out_scale=s_q)   # LayerNorm(x + y)
+
+In a decoder, with an int8 cache of keys and values in pages (kv_len: a sequence's
+cached tokens with the call's own; page_table: the numbers of its pages):
+
+    cache = torch.zeros(sl.cache_shape(n_pages, page_size, n_kv_heads, head_dim), dtype=torch.int8, device="cuda")
+    q = sl.cache_append(qkv, cache, page_table, seq_start, kv_len, max_new, n_heads, x_scale=s_qkv, q_scale=s_q,
+                        k_scale=s_k, v_scale=s_v, rope=sl.ROPE_HALF, inv_freq=inv_freq)
+    a = sl.cache_attention(q, cache, page_table, seq_start, kv_len, max_new, max_len, n_heads, q_scale=s_q,
+                           k_scale=s_k, v_scale=s_v, out_scale=s_a)      # causal=False: over an encoder's states
 """
 from __future__ import annotations
 
@@ -44,6 +53,7 @@ LAYOUT_ROWS, LAYOUT_T16X32 = 0, 1
 NORM_NONE, NORM_LAYER, NORM_RMS = 0, 1, 2
 GATE_NONE, GATE_CHANNEL, GATE_TOKEN, GATE_ELEMENT = 0, 1, 2, 3
 ACT_NONE, ACT_F32, ACT_I8 = 0, 1, 2
+ROPE_NONE, ROPE_HALF, ROPE_INTERLEAVED = 0, 1, 2
 KEY_BLOCK = 64  # keys of a selectable block
 
 SL_OK = 0
@@ -53,7 +63,7 @@ STATUS = {0: "SL_OK", -1: "SL_ERR_INVALID_ARG", -2: "SL_ERR_SHAPE", -3: "SL_ERR_
 # every symbol include/sparse_linear.h declares
 EXPORTS = ("sparse_linear_pack", "sparse_linear_pack_host", "sparse_linear_run", "sparse_linear_run_layout",
            "quantize_act", "quantize_act_layout", "residual_norm", "attention_run", "attention_select",
-           "attention_select_workspace",
+           "attention_select_workspace", "cache_append", "cache_attention", "cache_attention_workspace",
            "sparse_linear_unpack", "sparse_linear_info", "sparse_linear_export_bsr",
            "sparse_linear_tile_stats", "sparse_linear_free", "sl_status_string", "sl_last_error",
            "sl_abi_version", "sl_last_path", "sl_reload_env", "sl_gelu_table_codes")
@@ -93,13 +103,17 @@ def load() -> ctypes.CDLL:
     lib.attention_select.argtypes = [vp, vp, vp, i64, vp]
     lib.attention_select_workspace.argtypes = [vp]
     lib.attention_select_workspace.restype = i64
+    lib.cache_append.argtypes = [vp, vp]
+    lib.cache_attention.argtypes = [vp, vp]
+    lib.cache_attention_workspace.argtypes = [vp]
+    lib.cache_attention_workspace.restype = i64
     lib.sparse_linear_unpack.argtypes = [vp, vp]
     lib.sparse_linear_info.argtypes = [vp, vp, vp, vp]
     lib.sparse_linear_export_bsr.argtypes = [vp, vp, vp, vp]
     lib.sparse_linear_tile_stats.argtypes = [vp, vp, vp, vp, vp]
     for name in ("sparse_linear_pack", "sparse_linear_pack_host", "sparse_linear_run", "sparse_linear_run_layout",
                  "quantize_act", "quantize_act_layout", "residual_norm", "attention_run", "attention_select",
-                 "sparse_linear_unpack", "sparse_linear_info", "sparse_linear_export_bsr",
+                 "cache_append", "cache_attention", "sparse_linear_unpack", "sparse_linear_info", "sparse_linear_export_bsr",
                  "sparse_linear_tile_stats"):
         getattr(lib, name).restype = i32
     lib.sparse_linear_free.argtypes = [vp]
@@ -360,9 +374,11 @@ def quantize_act(x, scale: float, out=None, stream=None, layout: int = LAYOUT_RO
 
 # --- between the linears ------------------------------------------------------
 
-# sl_residual_norm_args and sl_attention_args, field by field
+# sl_residual_norm_args, sl_attention_args, sl_cache_append_args and sl_cache_attention_args, field by field
 _NORM_ARGS = struct.Struct("q10P9i5f0q")
 _ATTN_ARGS = struct.Struct("Pq4P10i3f0q")
+_APPEND_ARGS = struct.Struct("Pq7P13i5f0q")
+_CACHE_ARGS = struct.Struct("Pq6Pq14i5f0q")
 
 
 def _act_type(x, name: str, layout: int, shape) -> int:
@@ -552,4 +568,161 @@ def select_blocks(qkv, seq_start, max_len: int, n_heads: int, head_dim: int, top
     st = lib.attention_select(args, out.data_ptr(), work.data_ptr(), size, s)
     if st != SL_OK:
         _check(st, "attention_select")
+    return out
+
+
+# --- a decoder's cache ----------------------------------------------------------
+
+def cache_shape(n_pages: int, page_size: int, n_kv_heads: int, head_dim: int):
+    """Shape of a key-value cache: pages, keys and values, heads. Keys of a page and head are [page_size, head_dim],
+    values, in the same shape's memory, [page_size / 16, head_dim, 16]."""
+    return (n_pages, 2, n_kv_heads, page_size, head_dim)
+
+
+def _cache_args(x, name, cache, page_table, seq_start, kv_len):
+    """Checks of what cache_append and cache_attention share."""
+    torch = _torch or _torch_once()
+    i32 = torch.int32
+    if not x.is_cuda or not x.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous CUDA tensor")
+    if cache.dtype is not torch.int8 or cache.dim() != 5 or cache.shape[1] != 2 or not cache.is_contiguous():
+        raise ValueError("cache must be a contiguous int8 tensor of cache_shape()")
+    if page_table.dtype is not i32 or page_table.dim() != 2 or not page_table.is_contiguous():
+        raise ValueError("page_table must be a contiguous int32 tensor [n_seq, pages]")
+    if seq_start.dtype is not i32 or seq_start.dim() != 1 or not seq_start.is_contiguous() or \
+            kv_len.dtype is not i32 or kv_len.dim() != 1 or not kv_len.is_contiguous():
+        raise ValueError("seq_start and kv_len must be contiguous 1-D int32 tensors")
+    n_seq = kv_len.shape[0]
+    if seq_start.shape[0] != n_seq + 1 or page_table.shape[0] != n_seq:
+        raise ValueError("seq_start has n_seq + 1 entries, kv_len and page_table n_seq")
+    dev = x.get_device()
+    if cache.get_device() != dev or page_table.get_device() != dev or seq_start.get_device() != dev or \
+            kv_len.get_device() != dev:
+        raise ValueError(f"cache, page_table, seq_start and kv_len must be on {name}'s device")
+    return n_seq
+
+
+def _on_current(x, stream):
+    """The stream's number; the launch goes to the current device, which has to be x's (and the stream's)."""
+    torch = _torch
+    dev = x.get_device()
+    if stream is not None and stream.device_index != dev or torch._C._cuda_getDevice() != dev:
+        raise ValueError("the tensors' device must be the current one, and the stream's")
+    return _stream_ptr(stream)
+
+
+def cache_append(x, cache, page_table, seq_start, kv_len, max_new: int, n_heads: int, *, x_scale: float = 1.0,
+                 k_scale: float, v_scale: float, q_scale: Optional[float] = None, rope: int = ROPE_NONE, inv_freq=None,
+                 rope_factor: float = 1.0, positions=None, x_layout: int = LAYOUT_ROWS, q_layout: int = LAYOUT_ROWS,
+                 m_tokens: Optional[int] = None, out=None, stream=None):
+    """A QKV linear's output, [M, (n_heads + 2 n_kv_heads) * head_dim] fp32 or int8 codes of x_scale in x_layout, into
+    the pages of a cache (cache_shape; codes of k_scale and v_scale) and to query codes of q_scale, queries and keys
+    rotated by position.
+
+    Sequence s is tokens seq_start[s] .. seq_start[s+1]-1 (at most max_new, which sizes the launch), the last of its
+    kv_len[s] cached ones; page_table [n_seq, pages] names its pages (-1: none, not stored). inv_freq: fp32, one a
+    rotated pair (rope: ROPE_HALF pairs j with j + R / 2, ROPE_INTERLEAVED 2 j with 2 j + 1), angles position *
+    inv_freq; positions: int32 [M], default a token's slot; rope_factor multiplies both parts. n_heads may be 0 (an
+    encoder's keys and values). Returns the query codes [M, n_heads * head_dim] in q_layout, or None without q_scale.
+    Tokens of no sequence are left as they are."""
+    torch = _torch or _torch_once()
+    n_seq = _cache_args(x, "x", cache, page_table, seq_start, kv_len)
+    n_pages, _, n_kv, page_size, head_dim = cache.shape
+    cols = (n_heads + 2 * n_kv) * head_dim
+    x_type = ACT_F32 if x.dtype is torch.float32 else ACT_I8
+    if x_type == ACT_I8 and x.dtype is not torch.int8:
+        raise ValueError("x must be float32 or int8")
+    if x_layout == LAYOUT_T16X32:
+        if x_type == ACT_F32 or m_tokens is None:
+            raise ValueError("LAYOUT_T16X32 input is int8, and needs m_tokens")
+        if x.shape != t16x32_shape(m_tokens, cols):
+            raise ValueError(f"x must have shape {t16x32_shape(m_tokens, cols)}")
+    elif x.dim() != 2 or x.shape[1] != cols or (m_tokens is not None and m_tokens != x.shape[0]):
+        raise ValueError(f"x must be [{'M' if m_tokens is None else m_tokens}, {cols}]")
+    else:
+        m_tokens = x.shape[0]
+    q = None
+    if q_scale is not None:
+        shape = t16x32_shape(m_tokens, n_heads * head_dim) if q_layout == LAYOUT_T16X32 else (m_tokens, n_heads * head_dim)
+        if out is None:
+            q = torch.empty(shape, dtype=torch.int8, device=x.device)
+        else:
+            q = out
+            if q.dtype is not torch.int8 or q.shape != shape or not q.is_contiguous() or q.device != x.device:
+                raise ValueError(f"out must be a contiguous int8 tensor of shape {shape} on x's device")
+    rope_dim = freq = at = 0
+    if rope != ROPE_NONE:
+        if inv_freq is None or inv_freq.dtype is not torch.float32 or inv_freq.dim() != 1 or \
+                not inv_freq.is_contiguous() or inv_freq.device != x.device:
+            raise ValueError("inv_freq must be a contiguous 1-D float32 tensor on x's device")
+        rope_dim, freq = 2 * inv_freq.shape[0], inv_freq.data_ptr()
+        if positions is not None:
+            if positions.dtype is not torch.int32 or positions.shape != (m_tokens,) or \
+                    not positions.is_contiguous() or positions.device != x.device:
+                raise ValueError("positions must be a contiguous int32 tensor [M] on x's device")
+            at = positions.data_ptr()
+    args = _APPEND_ARGS.pack(
+        x.data_ptr(), m_tokens, seq_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), at, freq, cache.data_ptr(),
+        0 if q is None else q.data_ptr(), n_seq, max_new, page_table.shape[1], n_pages, page_size, x_type, x_layout, n_heads,
+        n_kv, head_dim, rope, rope_dim, q_layout, x_scale, rope_factor, 1.0 if q_scale is None else q_scale, k_scale, v_scale)
+    st = load().cache_append(args, _on_current(x, stream))
+    if st != SL_OK:
+        _check(st, "cache_append")
+    return q
+
+
+def cache_attention(q, cache, page_table, seq_start, kv_len, max_new: int, max_len: int, n_heads: int, *, q_scale: float,
+                    k_scale: float, v_scale: float, softmax_scale: Optional[float] = None, causal: bool = True,
+                    kind: int = EPI_I8, out_scale: float = 1.0, q_cols: Optional[int] = None,
+                    q_layout: int = LAYOUT_ROWS, y_layout: int = LAYOUT_ROWS, m_tokens: Optional[int] = None, out=None,
+                    stream=None):
+    """Attention of a call's tokens (query codes [M, n_heads * head_dim] of q_scale, or wider rows that begin with them:
+    q_cols, in the block layout) over what their sequences have in the cache: one token a sequence, some, or prompts.
+
+    Sequences as in cache_append; max_new and max_len, the largest of their tokens and of kv_len, size the launch. With
+    causal a token sees the slots up to its own, else all kv_len[s] (an encoder's states). softmax_scale: default
+    1 / sqrt(head_dim). Returns [M, n_heads * head_dim]: int8 codes of out_scale (EPI_I8, y_layout) or fp32 (EPI_F32); 0
+    where nothing is seen. Tokens of no sequence are left as they are."""
+    torch = _torch or _torch_once()
+    n_seq = _cache_args(q, "q", cache, page_table, seq_start, kv_len)
+    n_pages, _, n_kv, page_size, head_dim = cache.shape
+    if q.dtype is not torch.int8:
+        raise ValueError("q must be int8")
+    cols = n_heads * head_dim
+    if q_layout == LAYOUT_T16X32:
+        q_cols = cols if q_cols is None else q_cols
+        if m_tokens is None:
+            raise ValueError("m_tokens is required with LAYOUT_T16X32 input")
+        if q.shape != t16x32_shape(m_tokens, q_cols):
+            raise ValueError(f"q must have shape {t16x32_shape(m_tokens, q_cols)}")
+    elif q.dim() != 2 or (m_tokens is not None and m_tokens != q.shape[0]) or \
+            (q_cols is not None and q_cols != q.shape[1]) or q.shape[1] < cols:
+        raise ValueError(f"q must be [{'M' if m_tokens is None else m_tokens}, {cols} or more]")
+    else:
+        m_tokens, q_cols = q.shape
+    dt = _KIND_DTYPE.get(kind)
+    shape = t16x32_shape(m_tokens, cols) if y_layout == LAYOUT_T16X32 else (m_tokens, cols)
+    if out is None:
+        out = torch.empty(shape, dtype=dt, device=q.device)
+    elif out.dtype is not dt or out.shape != shape or not out.is_contiguous() or out.device != q.device:
+        raise ValueError("out has the wrong dtype/shape/device or is not contiguous")
+    scale = head_dim ** -0.5 if softmax_scale is None and head_dim else softmax_scale
+    fields = (n_seq, max_new, max_len, page_table.shape[1], n_pages, page_size, q_layout, q_cols, n_heads, n_kv, head_dim,
+              1 if causal else 0, kind, y_layout, q_scale, k_scale, v_scale, scale, out_scale)
+    head = (q.data_ptr(), m_tokens, seq_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), cache.data_ptr(),
+            out.data_ptr())
+    lib, s = load(), _on_current(q, stream)
+    args = _CACHE_ARGS.pack(*head, 0, 0, *fields)
+    size = lib.cache_attention_workspace(args)
+    if size:
+        # from the memory of the stream that uses it, which is not handed on before that work is done
+        if stream is None:
+            work = torch.empty(size, dtype=torch.uint8, device=q.device)
+        else:
+            with torch.cuda.stream(stream):
+                work = torch.empty(size, dtype=torch.uint8, device=q.device)
+        args = _CACHE_ARGS.pack(*head, work.data_ptr(), size, *fields)
+    st = lib.cache_attention(args, s)
+    if st != SL_OK:
+        _check(st, "cache_attention")
     return out

@@ -1,0 +1,573 @@
+// cache_append and cache_attention for few queries a sequence (gfx950).
+#include <hip/hip_runtime.h>
+#include <math.h>
+
+#include <algorithm>
+
+#include "encoder.h"
+#include "sl_device.h"
+
+namespace sl {
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// tokens first .. first + n - 1 of a call that belong to a sequence
+struct Tokens {
+    int32_t first, n;
+};
+__device__ __forceinline__ Tokens tokens_of(const int32_t *seq_start, int32_t s, int64_t m)
+{
+    const int32_t m32 = (int32_t)m;
+    const int32_t b = min(max(seq_start[s], 0), m32);
+    return {b, min(max(seq_start[s + 1], b), m32) - b};
+}
+
+// byte offset of feature c of token t
+__device__ __forceinline__ int64_t at(int64_t t, int32_t c, int32_t cols, int32_t cb)
+{
+    return cb ? t16x32_offset(t, c, cb) : t * cols + c;
+}
+
+// --- cache_append --------------------------------------------------------------
+
+struct AppendArgs {
+    sl_cache_append_args a;
+    int32_t cols, x_cb, q_cb, shift;  // 1 << shift: tokens of a page
+    int32_t quads, parts;             // workgroups along a sequence's tokens, and along its features
+    float fq, fk, fv;                 // from x's unit to the codes'
+};
+
+__device__ __forceinline__ f32x4 codes_to_float(uint32_t w)
+{
+    return f32x4{(float)(int8_t)w, (float)(int8_t)(w >> 8), (float)(int8_t)(w >> 16), (float)(int8_t)(w >> 24)};
+}
+
+__device__ __forceinline__ uint32_t codes_of(f32x4 v, float f)
+{
+    return pack_bytes(requant_bits(v[0], f), requant_bits(v[1], f), requant_bits(v[2], f), requant_bits(v[3], f));
+}
+
+// One workgroup: up to 4 consecutive slots (one word of a feature's values in the
+// cache) of one sequence, and a share of the features. VEC: rope_dim is a multiple
+// of 8, so that 4 features of a pair's halves lie together.
+template <bool F32, bool VEC>
+__global__ __launch_bounds__(256) void cache_append_kernel(const AppendArgs p)
+{
+    __shared__ __attribute__((aligned(16))) float cs[4][64], sn[4][64];
+    const sl_cache_append_args &a = p.a;
+    const int tid = threadIdx.x;
+    const int32_t part = (int32_t)(blockIdx.x % (uint32_t)p.parts);
+    const int32_t quad = (int32_t)(blockIdx.x / (uint32_t)p.parts % (uint32_t)p.quads);
+    const int32_t seq = (int32_t)(blockIdx.x / (uint32_t)p.parts / (uint32_t)p.quads);
+    const Tokens tk = tokens_of(a.seq_start, seq, a.m_tokens);
+    if (tk.n == 0) return;
+    const int32_t hd = a.head_dim, nh = a.n_heads, nkv = a.n_kv_heads, half = a.rope_kind ? a.rope_dim / 2 : 0;
+    const int32_t len = max(a.kv_len[seq], 0);
+    const int64_t p0 = (int64_t)len - tk.n;  // the first token's slot
+    const float *xf = static_cast<const float *>(a.x);
+    const int8_t *xc = static_cast<const int8_t *>(a.x);
+    const auto load4 = [&](int64_t t, int32_t c) {
+        if constexpr (F32)
+            return *reinterpret_cast<const f32x4 *>(xf + t * p.cols + c);
+        else
+            return codes_to_float(*reinterpret_cast<const uint32_t *>(xc + at(t, c, p.cols, p.x_cb)));
+    };
+    const auto load1 = [&](int64_t t, int32_t c) {
+        return F32 ? xf[t * p.cols + c] : (float)xc[at(t, c, p.cols, p.x_cb)];
+    };
+    for (int64_t q4 = ((p0 >> 2) + quad) * 4; q4 < len; q4 += (int64_t)p.quads * 4) {
+        const int64_t lo = max(q4, p0), hi = min(q4 + 4, (int64_t)len);
+        const int32_t n = (int32_t)(hi - lo), skip = (int32_t)(lo - q4);
+        const int64_t t0 = tk.first + (lo - p0);
+        if (half) {
+            __syncthreads();
+            for (int i = tid; i < n * half; i += 256) {
+                const int32_t j = i / half, w = i % half;
+                const double pos = a.positions ? (double)a.positions[t0 + j] : (double)(lo + j);
+                const double turns = pos * (double)a.inv_freq[w] * 0.15915494309189533577;
+                float s, c;
+                sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
+                cs[j][w] = c * a.rope_factor;
+                sn[j][w] = s * a.rope_factor;
+            }
+            __syncthreads();
+        }
+        int8_t *page = nullptr;
+        const int64_t entry = q4 >> p.shift;
+        const int32_t in_page = (int32_t)(q4 & ((1 << p.shift) - 1));
+        if (q4 >= 0 && entry < a.max_pages) {
+            const int32_t number = a.page_table[(int64_t)seq * a.max_pages + entry];
+            if ((uint32_t)number < (uint32_t)a.n_pages)
+                page = a.cache + (int64_t)number * (2 * nkv) * ((int64_t)hd << p.shift);
+        }
+        // queries and keys: 8 features (VEC) or 2 a thread
+        constexpr int U = VEC ? 8 : 2;
+        const int32_t units = (nh + nkv) * (hd / U), all = n * units;
+        const auto store = [&](int32_t j, int32_t head, int32_t c, auto code) {
+            using T = decltype(code);
+            if (head < nh) {
+                if (a.q) *reinterpret_cast<T *>(a.q + at(t0 + j, head * hd + c, nh * hd, p.q_cb)) = code;
+            } else if (page) {
+                *reinterpret_cast<T *>(page + (int64_t)(((head - nh) << p.shift) + in_page + skip + j) * hd + c) = code;
+            }
+        };
+        for (int32_t i = part * 256 + tid; i < all; i += p.parts * 256) {
+            const int32_t j = i / units, u = i % units, head = u / (hd / U), k = u % (hd / U);
+            const int64_t t = t0 + j;
+            const float f = head < nh ? p.fq : p.fk;
+            if constexpr (VEC) {
+                const bool turned = 4 * k < half;
+                const bool split = turned && a.rope_kind == SL_ROPE_HALF;
+                const int32_t c0 = split ? 4 * k : 8 * k, c1 = split ? 4 * k + half : 8 * k + 4;
+                f32x4 v0 = load4(t, head * hd + c0), v1 = load4(t, head * hd + c1);
+                if (turned) {
+                    const f32x4 c = *reinterpret_cast<const f32x4 *>(&cs[j][4 * k]);
+                    const f32x4 s = *reinterpret_cast<const f32x4 *>(&sn[j][4 * k]);
+                    const f32x4 x = split ? v0 : f32x4{v0[0], v0[2], v1[0], v1[2]};
+                    const f32x4 y = split ? v1 : f32x4{v0[1], v0[3], v1[1], v1[3]};
+                    const f32x4 x2 = x * c - y * s, y2 = y * c + x * s;
+                    v0 = split ? x2 : f32x4{x2[0], y2[0], x2[1], y2[1]};
+                    v1 = split ? y2 : f32x4{x2[2], y2[2], x2[3], y2[3]};
+                }
+                store(j, head, c0, codes_of(v0, f));
+                store(j, head, c1, codes_of(v1, f));
+            } else {
+                const bool turned = k < half;
+                const bool split = turned && a.rope_kind == SL_ROPE_HALF;
+                const int32_t c0 = split ? k : 2 * k, c1 = split ? k + half : 2 * k + 1;
+                float x = load1(t, head * hd + c0), y = load1(t, head * hd + c1);
+                if (turned) {
+                    const float c = cs[j][k], s = sn[j][k], x2 = x * c - y * s;
+                    y = y * c + x * s;
+                    x = x2;
+                }
+                store(j, head, c0, (int8_t)requant_bits(x, f));
+                store(j, head, c1, (int8_t)requant_bits(y, f));
+            }
+        }
+        if (!page) continue;
+        // values: 4 features of all the slots a thread
+        int8_t *values = page + (int64_t)nkv * ((int64_t)hd << p.shift);
+        for (int32_t i = part * 256 + tid; i < nkv * (hd / 4); i += p.parts * 256) {
+            const int32_t head = i / (hd / 4), c = i % (hd / 4) * 4;
+            int8_t *to = values + ((int64_t)((head << p.shift) + (in_page & ~15)) * hd + c * 16 + (in_page & 15));
+            uint32_t w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                w[j] = j < n ? codes_of(load4(t0 + j, (nh + nkv + head) * hd + c), p.fv) : 0;
+            if (n == 4) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    *reinterpret_cast<uint32_t *>(to + 16 * e) =
+                        pack_bytes(w[0] >> (8 * e), w[1] >> (8 * e), w[2] >> (8 * e), w[3] >> (8 * e));
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (j < n) to[16 * e + skip + j] = (int8_t)(w[j] >> (8 * e));
+            }
+        }
+    }
+}
+
+// --- cache_attention, few queries a sequence ---------------------------------------
+
+constexpr int kWaves = 4;  // of a workgroup, which share its keys
+
+struct CacheArgs {
+    const int8_t *q, *cache;
+    const int32_t *seq_start, *kv_len, *page_table;
+    void *y;
+    float *work;
+    int64_t m;
+    int64_t n_items;
+    int32_t n_seq, tiles, splits, split_keys;
+    int32_t n_heads, n_kv, group, hd, q_cols, q_cb, y_cb, shift, max_pages, n_pages, causal, y_f32;
+    float c2, vs, inv_so;
+};
+
+// floats of a part's record in the workspace: 16 queries' m, l and O
+__host__ __device__ constexpr int64_t record(int hd) { return 16 * (int64_t)(hd + 2); }
+
+__device__ __forceinline__ int quad_max(int v)  // over lanes 16 and 32 apart
+{
+    const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = max((int)a[0], (int)a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return max((int)b[0], (int)b[1]);
+}
+__device__ __forceinline__ float quad_sum(float v)
+{
+    int i = __float_as_int(v);
+    const auto a = __builtin_amdgcn_permlane16_swap(i, i, false, false);
+    i = __float_as_int(__int_as_float(a[0]) + __int_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(i, i, false, false);
+    return __int_as_float(b[0]) + __int_as_float(b[1]);
+}
+
+// A weight of 0 .. 1 times kLargest plus kDigits is a float whose mantissa is the weight's whole number + 0x8080: its low
+// three bytes are three digits to the base 256, the lower two of them 128 too large.
+constexpr float kDigits = 8388608.0f + 32896.0f;
+constexpr uint32_t kDigitsBits = 0x4B008080u;
+constexpr float kLargest = 8355000.0f;  // (and 2^23 - 0x8080 more than it, by enough for an exponential over 1)
+constexpr int32_t kNone = -(1 << 30);  // m without a key
+
+// One output row's share: query row, 4 features from c on
+__device__ __forceinline__ void store_row(const CacheArgs &a, int64_t tok, int32_t head, int32_t c, f32x4 v, float l)
+{
+    const float g = l > 0.0f ? a.vs / l : 0.0f;
+    const int32_t cols = a.n_heads * a.hd;
+    if (a.y_f32)
+        *reinterpret_cast<f32x4 *>(static_cast<float *>(a.y) + tok * cols + head * a.hd + c) = v * g;
+    else
+        *reinterpret_cast<uint32_t *>(static_cast<int8_t *>(a.y) + at(tok, head * a.hd + c, cols, a.y_cb)) =
+            codes_of(v, g * a.inv_so);
+}
+
+template <int F, int KG>
+__global__ __launch_bounds__(64 * kWaves) void cache_split_kernel(const CacheArgs a)
+{
+    constexpr int N = (F + 3) / 4, HD = 16 * F;
+    __shared__ __attribute__((aligned(16))) float parts[kWaves][F * 4][64];
+    __shared__ int32_t ms[kWaves][16];
+    __shared__ float ls[kWaves][16];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, h = lane >> 4;
+    const uint32_t item = (uint32_t)xcd_work_index(blockIdx.x, a.n_items);
+    const int32_t split = (int32_t)(item % (uint32_t)a.splits);
+    const int32_t tile0 = (int32_t)(item / (uint32_t)a.splits % (uint32_t)a.tiles);
+    const uint32_t sh = item / (uint32_t)a.splits / (uint32_t)a.tiles;
+    const int32_t kv = (int32_t)(sh % (uint32_t)a.n_kv), seq = (int32_t)(sh / (uint32_t)a.n_kv);
+    const Tokens tk = tokens_of(a.seq_start, seq, a.m);
+    const int64_t rows = (int64_t)tk.n * a.group;
+    const int32_t len = max(a.kv_len[seq], 0);
+    const int32_t cached = (int32_t)min((int64_t)len, (int64_t)a.max_pages << a.shift);
+    const int32_t *table = a.page_table + (int64_t)seq * a.max_pages;
+    const int64_t head_bytes = (int64_t)HD << a.shift, page_bytes = 2 * a.n_kv * head_bytes;
+    const int8_t *keys = a.cache + kv * head_bytes, *values = keys + a.n_kv * head_bytes;
+    const int32_t last_entry = a.max_pages - 1, in_mask = (1 << a.shift) - 1;
+
+    for (int64_t tile = tile0; tile * 16 < rows; tile += a.tiles) {
+        const bool whole = a.splits == 1 || tile >= a.tiles;  // this workgroup alone sees all keys
+        if (whole && split) continue;
+        const int64_t row = tile * 16 + r;
+        const bool real = row < rows;
+        const int32_t i = real ? (int32_t)(row / a.group) : 0, head = kv * a.group + (int32_t)(real ? row % a.group : 0);
+        const int32_t limit = !real ? 0 : a.causal ? min(len - tk.n + i + 1, cached) : cached;
+        const int64_t last_row = min(tile * 16 + 15, rows - 1);
+        const int32_t most = a.causal ? min(len - tk.n + (int32_t)(last_row / a.group) + 1, cached) : cached;
+        const int32_t k0 = whole ? 0 : split * a.split_keys;
+        const int32_t k1 = whole || split == a.splits - 1 ? most : min(most, k0 + a.split_keys);
+        if (!whole && k0 >= most && split) continue;  // (part 0 says that there is none)
+
+        i32x4 q[N];
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            q[n] = i32x4{0, 0, 0, 0};
+            if (real && 64 * n + 16 * h < HD)
+                q[n] = *reinterpret_cast<const i32x4 *>(
+                    a.q + at((int64_t)tk.first + i, head * HD + 64 * n + 16 * h, a.q_cols, a.q_cb));
+        }
+        f32x4 o[F];
+#pragma unroll
+        for (int f = 0; f < F; ++f) o[f] = f32x4{0, 0, 0, 0};
+        float l = 0.0f;
+        int32_t m = kNone;
+
+        for (int32_t kb = k0 + wave * 64 * KG; kb < k1; kb += kWaves * 64 * KG) {
+            i32x4 kr[KG][4][N], vr[KG][F];
+            int32_t seen[KG];  // of the lane's 16 keys of a group of 64: those before `limit`
+#pragma unroll
+            for (int g = 0; g < KG; ++g) {
+                // key 16 (x / 4) + 4 t + x % 4 of the group is row x of score tile t, so that a lane's scores are
+                // those of the 16 keys whose values it takes
+                const int32_t tk0 = kb + 64 * g + 16 * (r >> 2), tv0 = kb + 64 * g + 16 * h;
+                int32_t pk = table[min(tk0 >> a.shift, last_entry)], pv = table[min(tv0 >> a.shift, last_entry)];
+                const bool there = (uint32_t)pv < (uint32_t)a.n_pages;
+                seen[g] = there ? limit - tv0 : 0;
+                pk = (uint32_t)pk < (uint32_t)a.n_pages ? pk : 0;
+                pv = there ? pv : 0;
+                const int8_t *ka = keys + pk * page_bytes + ((tk0 & in_mask) + (r & 3)) * HD;
+                const int8_t *va = values + pv * page_bytes + ((tv0 & in_mask) * HD + r * 16);
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int n = 0; n < N; ++n)
+                        kr[g][t][n] = *reinterpret_cast<const i32x4 *>(ka + 4 * t * HD + (64 * n + 16 * h < HD ? 64 * n + 16 * h : 0));
+#pragma unroll
+                for (int f = 0; f < F; ++f) vr[g][f] = *reinterpret_cast<const i32x4 *>(va + 256 * f);
+            }
+            i32x4 s[KG][4];
+#pragma unroll
+            for (int g = 0; g < KG; ++g)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    s[g][t] = i32x4{0, 0, 0, 0};
+#pragma unroll
+                    for (int n = 0; n < N; ++n)
+                        s[g][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(kr[g][t][n], q[n], s[g][t], 0, 0, 0);
+                }
+            int32_t top = kNone;
+#pragma unroll
+            for (int g = 0; g < KG; ++g)
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if (4 * t + e >= seen[g]) s[g][t][e] = kNone;
+                        top = max(top, s[g][t][e]);
+                    }
+            top = quad_max(top);
+            uint32_t sum = 0;
+            i32x4 d0[KG], d1[KG], d2[KG];
+#pragma unroll
+            for (int g = 0; g < KG; ++g)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float p = __builtin_amdgcn_exp2f((float)(s[g][t][e] - top) * a.c2);
+                        w[e] = __float_as_uint(fmaf(4 * t + e < seen[g] ? p : 0.0f, kLargest, kDigits));
+                        sum += w[e] - kDigitsBits;
+                    }
+                    const uint32_t low01 = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u);
+                    const uint32_t low23 = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u);
+                    const uint32_t top01 = __builtin_amdgcn_perm(w[1], w[0], 0x0c0c0602u);
+                    const uint32_t top23 = __builtin_amdgcn_perm(w[3], w[2], 0x0c0c0602u);
+                    d0[g][t] = (int)(__builtin_amdgcn_perm(low23, low01, 0x05040100u) ^ 0x80808080u);
+                    d1[g][t] = (int)(__builtin_amdgcn_perm(low23, low01, 0x07060302u) ^ 0x80808080u);
+                    d2[g][t] = (int)__builtin_amdgcn_perm(top23, top01, 0x05040100u);
+                }
+            const int32_t now = max(m, top);
+            const float fo = __builtin_amdgcn_exp2f((float)(m - now) * a.c2);
+            const float fb = __builtin_amdgcn_exp2f((float)(top - now) * a.c2);
+            m = now;
+            l = l * fo + fb * (float)sum;
+#pragma unroll
+            for (int f = 0; f < F; ++f) {
+                i32x4 c0 = {0, 0, 0, 0}, c1 = {0, 0, 0, 0}, c2 = {0, 0, 0, 0};
+#pragma unroll
+                for (int g = 0; g < KG; ++g) {
+                    c0 = __builtin_amdgcn_mfma_i32_16x16x64_i8(vr[g][f], d0[g], c0, 0, 0, 0);
+                    c1 = __builtin_amdgcn_mfma_i32_16x16x64_i8(vr[g][f], d1[g], c1, 0, 0, 0);
+                    c2 = __builtin_amdgcn_mfma_i32_16x16x64_i8(vr[g][f], d2[g], c2, 0, 0, 0);
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float v = fmaf((float)c2[e], 65536.0f, (float)(c1[e] * 256 + c0[e]));
+                    o[f][e] = o[f][e] * fo + v * fb;
+                }
+            }
+        }
+        // the waves' m, l and O together
+        l = quad_sum(l);
+        if (h == 0) {
+            ms[wave][r] = m;
+            ls[wave][r] = l;
+        }
+        __syncthreads();
+        int32_t mm = ms[0][r];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) mm = max(mm, ms[w][r]);
+        const float fw = __builtin_amdgcn_exp2f((float)(m - mm) * a.c2);
+#pragma unroll
+        for (int f = 0; f < F; ++f)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) parts[wave][4 * f + e][lane] = o[f][e] * fw;
+        float sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) sum += ls[w][r] * __builtin_amdgcn_exp2f((float)(ms[w][r] - mm) * a.c2);
+        __syncthreads();
+        float *rec = whole ? nullptr : a.work + ((int64_t)(sh * a.tiles + tile) * a.splits + split) * record(HD);
+        if (rec && wave == 0 && h == 0) {
+            reinterpret_cast<int32_t *>(rec)[r] = mm;
+            rec[16 + r] = sum;
+        }
+        for (int f = wave; f < F; f += kWaves) {
+            f32x4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[e] = parts[0][4 * f + e][lane];
+#pragma unroll
+                for (int w = 1; w < kWaves; ++w) v[e] += parts[w][4 * f + e][lane];
+            }
+            if (!real) continue;
+            if (rec)
+                *reinterpret_cast<f32x4 *>(rec + 32 + r * HD + 16 * f + 4 * h) = v;
+            else
+                store_row(a, (int64_t)tk.first + i, head, 16 * f + 4 * h, v, sum);
+        }
+        __syncthreads();
+    }
+}
+
+// The parts of a tile of 16 queries together. One wave a query: a lane 4 features.
+__global__ __launch_bounds__(256) void cache_join_kernel(const CacheArgs a)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t item = blockIdx.x;
+    const int32_t tile = (int32_t)(item % (uint32_t)a.tiles);
+    const uint32_t sh = item / (uint32_t)a.tiles;
+    const int32_t kv = (int32_t)(sh % (uint32_t)a.n_kv), seq = (int32_t)(sh / (uint32_t)a.n_kv);
+    const Tokens tk = tokens_of(a.seq_start, seq, a.m);
+    const int64_t rows = (int64_t)tk.n * a.group;
+    const int32_t len = max(a.kv_len[seq], 0);
+    const int32_t cached = (int32_t)min((int64_t)len, (int64_t)a.max_pages << a.shift);
+    const int64_t last_row = min((int64_t)tile * 16 + 15, rows - 1);
+    const int32_t most = a.causal ? min(len - tk.n + (int32_t)(last_row / a.group) + 1, cached) : cached;
+    const int32_t n = min(a.splits, max(1, (most + a.split_keys - 1) / a.split_keys));
+    const float *rec = a.work + (int64_t)item * a.splits * record(a.hd);
+    for (int r = wave; r < 16; r += 4) {
+        const int64_t row = (int64_t)tile * 16 + r;
+        if (row >= rows) return;
+        int32_t mm = kNone;
+        for (int s = lane; s < n; s += 64) mm = max(mm, reinterpret_cast<const int32_t *>(rec + s * record(a.hd))[r]);
+#pragma unroll
+        for (int d = 32; d; d >>= 1) mm = max(mm, __shfl_xor(mm, d));
+        float l = 0.0f;
+        f32x4 o = {0, 0, 0, 0};
+        const int c = 4 * lane;
+        for (int s = 0; s < n; ++s) {
+            const float *p = rec + s * record(a.hd);
+            const float f = __builtin_amdgcn_exp2f((float)(reinterpret_cast<const int32_t *>(p)[r] - mm) * a.c2);
+            l += p[16 + r] * f;
+            if (c < a.hd) o += *reinterpret_cast<const f32x4 *>(p + 32 + r * a.hd + c) * f;
+        }
+        if (c < a.hd)
+            store_row(a, (int64_t)tk.first + (int32_t)(row / a.group), kv * a.group + (int32_t)(row % a.group), c, o, l);
+    }
+}
+
+struct Plan {
+    int64_t tiles;
+    int32_t splits, split_keys;
+};
+Plan plan_of(const sl_cache_attention_args &a)
+{
+    const int32_t group = a.n_heads / a.n_kv_heads;
+    Plan p{((int64_t)a.max_new * group + 15) / 16, 1, 0};
+    const double all = (double)a.n_seq * a.n_kv_heads * (double)p.tiles;  // (a product of whole numbers may not fit)
+    if (all >= 512) return p;
+    const int64_t items = (int64_t)all;
+    const int64_t want = std::min<int64_t>((512 + items - 1) / items, ((int64_t)a.max_len + 255) / 256);
+    if (want > 1) {
+        p.split_keys = (int32_t)((((int64_t)a.max_len + want - 1) / want + 255) / 256 * 256);
+        p.splits = (int32_t)(((int64_t)a.max_len + p.split_keys - 1) / p.split_keys);
+    }
+    return p;
+}
+
+template <int F>
+sl_status launch_split(const CacheArgs &a, hipStream_t s)
+{
+    hipLaunchKernelGGL((cache_split_kernel<F, 2>), dim3((uint32_t)a.n_items), dim3(64 * kWaves), 0, s, a);
+    HIP_TRY(hipGetLastError());
+    return SL_OK;
+}
+
+}  // namespace
+
+int64_t cache_attention_bytes(const sl_cache_attention_args &a)
+{
+    const Plan p = plan_of(a);
+    if (p.splits == 1) return 0;
+    return (int64_t)a.n_seq * a.n_kv_heads * p.tiles * p.splits * record(a.head_dim) * 4;
+}
+
+sl_status launch_cache_append(const sl_cache_append_args &args, void *stream)
+{
+    AppendArgs p{};
+    p.a = args;
+    p.cols = (args.n_heads + 2 * args.n_kv_heads) * args.head_dim;
+    const bool f32 = args.x_type == SL_ACT_F32;
+    p.x_cb = !f32 && args.x_layout == SL_LAYOUT_T16X32 ? (p.cols + 31) / 32 : 0;
+    p.q_cb = args.q_layout == SL_LAYOUT_T16X32 ? (args.n_heads * args.head_dim + 31) / 32 : 0;
+    p.shift = __builtin_ctz(args.page_size);
+    const auto factor = [&](float scale) { return f32 ? 1.0f / scale : (float)((double)args.x_scale / scale); };
+    p.fq = factor(args.q_scale);
+    p.fk = factor(args.k_scale);
+    p.fv = factor(args.v_scale);
+    p.quads = (args.max_new + 6) / 4;
+    const int64_t groups = (int64_t)p.quads * args.n_seq;
+    const bool vec = args.rope_kind == SL_ROPE_NONE || args.rope_dim % 8 == 0;
+    // (a part of the features has a unit a thread at least)
+    p.parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>(512 / groups, p.cols / 8 / 256));
+    const int64_t items = groups * p.parts;
+    if (items > 0x7fffffff / 256) {
+        set_error("too many work items for one launch");
+        return SL_ERR_UNSUPPORTED;
+    }
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    const dim3 grid((uint32_t)items), block(256);
+    if (f32 && vec)
+        hipLaunchKernelGGL((cache_append_kernel<true, true>), grid, block, 0, s, p);
+    else if (f32)
+        hipLaunchKernelGGL((cache_append_kernel<true, false>), grid, block, 0, s, p);
+    else if (vec)
+        hipLaunchKernelGGL((cache_append_kernel<false, true>), grid, block, 0, s, p);
+    else
+        hipLaunchKernelGGL((cache_append_kernel<false, false>), grid, block, 0, s, p);
+    HIP_TRY(hipGetLastError());
+    return SL_OK;
+}
+
+sl_status launch_cache_attention(const sl_cache_attention_args &args, void *stream)
+{
+    CacheArgs a{};
+    a.q = args.q;
+    a.cache = args.cache;
+    a.seq_start = args.seq_start;
+    a.kv_len = args.kv_len;
+    a.page_table = args.page_table;
+    a.y = args.y;
+    a.work = static_cast<float *>(args.workspace);
+    a.m = args.m_tokens;
+    const Plan p = plan_of(args);
+    if ((double)args.n_seq * args.n_kv_heads * (double)p.tiles * p.splits > 0x7fffffff / (64 * kWaves)) {
+        set_error("too many work items for one launch");
+        return SL_ERR_UNSUPPORTED;
+    }
+    a.n_seq = args.n_seq;
+    a.tiles = (int32_t)p.tiles;
+    a.splits = p.splits;
+    a.split_keys = p.split_keys;
+    a.n_heads = args.n_heads;
+    a.n_kv = args.n_kv_heads;
+    a.group = args.n_heads / args.n_kv_heads;
+    a.hd = args.head_dim;
+    a.q_cols = args.q_cols;
+    a.q_cb = args.q_layout == SL_LAYOUT_T16X32 ? (args.q_cols + 31) / 32 : 0;
+    a.y_cb = args.y_layout == SL_LAYOUT_T16X32 ? (args.n_heads * args.head_dim + 31) / 32 : 0;
+    a.shift = __builtin_ctz(args.page_size);
+    a.max_pages = args.n_pages ? args.max_pages : 0;  // (no page: nothing is read)
+    a.n_pages = args.n_pages;
+    a.causal = args.causal;
+    a.y_f32 = args.kind == SL_EPI_F32;
+    a.c2 = (float)((double)args.q_scale * args.k_scale * args.softmax_scale * 1.4426950408889634);
+    a.vs = args.v_scale;
+    a.inv_so = a.y_f32 ? 1.0f : 1.0f / args.out_scale;
+    a.n_items = (int64_t)a.n_seq * a.n_kv * a.tiles * a.splits;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    sl_status st;
+    switch (a.hd / 16) {
+    case 1: st = launch_split<1>(a, s); break;
+    case 2: st = launch_split<2>(a, s); break;
+    case 3: st = launch_split<3>(a, s); break;
+    case 4: st = launch_split<4>(a, s); break;
+    case 5: st = launch_split<5>(a, s); break;
+    case 6: st = launch_split<6>(a, s); break;
+    case 7: st = launch_split<7>(a, s); break;
+    default: st = launch_split<8>(a, s); break;
+    }
+    if (st == SL_OK && a.splits > 1) {
+        hipLaunchKernelGGL(cache_join_kernel, dim3((uint32_t)(a.n_items / a.splits)), dim3(256), 0, s, a);
+        HIP_TRY(hipGetLastError());
+    }
+    if (st == SL_OK) set_last_path("cache split %d,%d", a.hd, a.splits);
+    return st;
+}
+
+}  // namespace sl
