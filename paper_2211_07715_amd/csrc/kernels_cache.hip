@@ -3,6 +3,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "encoder.h"
 #include "sl_device.h"
@@ -176,6 +177,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(const AppendArgs p)
 // --- cache_attention, few queries a sequence ---------------------------------------
 
 constexpr int kWaves = 4;  // of a workgroup, which share its keys
+constexpr int kSpan = 64;  // keys that a wave takes at a time
 
 struct CacheArgs {
     const int8_t *q, *cache;
@@ -183,10 +185,9 @@ struct CacheArgs {
     void *y;
     float *work;
     int64_t m;
-    int64_t n_items;
     int32_t n_seq, tiles, splits, split_keys;
-    int32_t n_heads, n_kv, group, hd, q_cols, q_cb, y_cb, shift, max_pages, n_pages, causal, y_f32;
-    float c2, vs, inv_so;
+    int32_t n_heads, n_kv, group, hd, q_cols, q_cb, y_cb, shift, max_pages, n_pages, causal, y_f32, join_rows, seq0;
+    float c2, vs, inv_so, inv_group;
 };
 
 // floats of a part's record in the workspace: 16 queries' m, l and O
@@ -227,37 +228,44 @@ __device__ __forceinline__ void store_row(const CacheArgs &a, int64_t tok, int32
             codes_of(v, g * a.inv_so);
 }
 
-template <int F, int KG>
-__global__ __launch_bounds__(64 * kWaves) void cache_split_kernel(const CacheArgs a)
+template <int F>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(3))) void cache_split_kernel(const CacheArgs a)
 {
-    constexpr int N = (F + 3) / 4, HD = 16 * F;
+    constexpr int N = (F + 3) / 4, HD = 16 * F, FB = 2;
     __shared__ __attribute__((aligned(16))) float parts[kWaves][F * 4][64];
     __shared__ int32_t ms[kWaves][16];
     __shared__ float ls[kWaves][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, h = lane >> 4;
-    const uint32_t item = (uint32_t)xcd_work_index(blockIdx.x, a.n_items);
-    const int32_t split = (int32_t)(item % (uint32_t)a.splits);
-    const int32_t tile0 = (int32_t)(item / (uint32_t)a.splits % (uint32_t)a.tiles);
-    const uint32_t sh = item / (uint32_t)a.splits / (uint32_t)a.tiles;
-    const int32_t kv = (int32_t)(sh % (uint32_t)a.n_kv), seq = (int32_t)(sh / (uint32_t)a.n_kv);
+    const int32_t split = blockIdx.z, seq = a.seq0 + blockIdx.y;
+    const int32_t kv = a.tiles == 1 ? blockIdx.x : blockIdx.x / (uint32_t)a.tiles, tile0 = blockIdx.x - kv * a.tiles;
+    const int32_t *table = a.page_table + (int64_t)seq * a.max_pages;
+    const int32_t last_entry = a.max_pages - 1, in_mask = (1 << a.shift) - 1;
+    // pages of the 16 keys that the lane's row of the scores' left operand and its values come from
+    int32_t pk = -1, pv = -1;
+    const auto entries = [&](int32_t kb) __attribute__((always_inline)) {
+        pk = table[min((kb + 16 * (r >> 2)) >> a.shift, last_entry)];
+        pv = table[min((kb + 16 * h) >> a.shift, last_entry)];
+    };
+    if (a.max_pages) entries(split * a.split_keys + wave * kSpan);  // (on their way with the lengths)
     const Tokens tk = tokens_of(a.seq_start, seq, a.m);
     const int64_t rows = (int64_t)tk.n * a.group;
     const int32_t len = max(a.kv_len[seq], 0);
     const int32_t cached = (int32_t)min((int64_t)len, (int64_t)a.max_pages << a.shift);
-    const int32_t *table = a.page_table + (int64_t)seq * a.max_pages;
     const int64_t head_bytes = (int64_t)HD << a.shift, page_bytes = 2 * a.n_kv * head_bytes;
     const int8_t *keys = a.cache + kv * head_bytes, *values = keys + a.n_kv * head_bytes;
-    const int32_t last_entry = a.max_pages - 1, in_mask = (1 << a.shift) - 1;
 
     for (int64_t tile = tile0; tile * 16 < rows; tile += a.tiles) {
         const bool whole = a.splits == 1 || tile >= a.tiles;  // this workgroup alone sees all keys
         if (whole && split) continue;
-        const int64_t row = tile * 16 + r;
-        const bool real = row < rows;
-        const int32_t i = real ? (int32_t)(row / a.group) : 0, head = kv * a.group + (int32_t)(real ? row % a.group : 0);
+        // row r: token i, head of the group
+        const int32_t i0 = tile ? (int32_t)(tile * 16 / a.group) : 0, g0 = (int32_t)(tile * 16 - (int64_t)i0 * a.group) + r;
+        const bool real = tile * 16 + r < rows;
+        const int32_t di = a.group >= 16 ? (g0 >= a.group ? 1 : 0) : (int32_t)(((float)g0 + 0.5f) * a.inv_group);  // (g0 < 32)
+        const int32_t i = i0 + di, head = kv * a.group + (g0 - di * a.group);
         const int32_t limit = !real ? 0 : a.causal ? min(len - tk.n + i + 1, cached) : cached;
-        const int64_t last_row = min(tile * 16 + 15, rows - 1);
-        const int32_t most = a.causal ? min(len - tk.n + (int32_t)(last_row / a.group) + 1, cached) : cached;
+        // (a tile's queries see no more keys than its last one, lane 15's or the last real one's)
+        const int32_t last = min(__builtin_amdgcn_readlane(i, 15), tk.n - 1);
+        const int32_t most = a.causal ? min(len - tk.n + last + 1, cached) : cached;
         const int32_t k0 = whole ? 0 : split * a.split_keys;
         const int32_t k1 = whole || split == a.splits - 1 ? most : min(most, k0 + a.split_keys);
         if (!whole && k0 >= most && split) continue;  // (part 0 says that there is none)
@@ -276,90 +284,108 @@ __global__ __launch_bounds__(64 * kWaves) void cache_split_kernel(const CacheArg
         float l = 0.0f;
         int32_t m = kNone;
 
-        for (int32_t kb = k0 + wave * 64 * KG; kb < k1; kb += kWaves * 64 * KG) {
-            i32x4 kr[KG][4][N], vr[KG][F];
-            int32_t seen[KG];  // of the lane's 16 keys of a group of 64: those before `limit`
-#pragma unroll
-            for (int g = 0; g < KG; ++g) {
-                // key 16 (x / 4) + 4 t + x % 4 of the group is row x of score tile t, so that a lane's scores are
-                // those of the 16 keys whose values it takes
-                const int32_t tk0 = kb + 64 * g + 16 * (r >> 2), tv0 = kb + 64 * g + 16 * h;
-                int32_t pk = table[min(tk0 >> a.shift, last_entry)], pv = table[min(tv0 >> a.shift, last_entry)];
-                const bool there = (uint32_t)pv < (uint32_t)a.n_pages;
-                seen[g] = there ? limit - tv0 : 0;
-                pk = (uint32_t)pk < (uint32_t)a.n_pages ? pk : 0;
-                pv = there ? pv : 0;
-                const int8_t *ka = keys + pk * page_bytes + ((tk0 & in_mask) + (r & 3)) * HD;
-                const int8_t *va = values + pv * page_bytes + ((tv0 & in_mask) * HD + r * 16);
+        const int32_t kb0 = k0 + wave * kSpan;
+        if (kb0 < k1 && tile != tile0) entries(kb0);
+        for (int32_t kb = kb0; kb < k1; kb += kWaves * kSpan) {
+            // key 16 (x / 4) + 4 t + x % 4 of the span is row x of score tile t, so that a lane's scores are those of
+            // the 16 keys whose values it takes
+            i32x4 kr[4][N], vr[F];
+            {
+                const int32_t page = (uint32_t)pk < (uint32_t)a.n_pages ? pk : 0;
+                const int8_t *from = keys + page * page_bytes + (((kb + 16 * (r >> 2)) & in_mask) + (r & 3)) * HD;
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
 #pragma unroll
                     for (int n = 0; n < N; ++n)
-                        kr[g][t][n] = *reinterpret_cast<const i32x4 *>(ka + 4 * t * HD + (64 * n + 16 * h < HD ? 64 * n + 16 * h : 0));
-#pragma unroll
-                for (int f = 0; f < F; ++f) vr[g][f] = *reinterpret_cast<const i32x4 *>(va + 256 * f);
+                        kr[t][n] = *reinterpret_cast<const i32x4 *>(from + 4 * t * HD + (64 * n + 16 * h < HD ? 64 * n + 16 * h : 0));
             }
-            i32x4 s[KG][4];
+            const bool there = (uint32_t)pv < (uint32_t)a.n_pages;
+            {
+                const int32_t page = there ? pv : 0;
+                const int8_t *from = values + page * page_bytes + (((kb + 16 * h) & in_mask) * HD + r * 16);
 #pragma unroll
-            for (int g = 0; g < KG; ++g)
+                for (int f = 0; f < F; ++f) vr[f] = *reinterpret_cast<const i32x4 *>(from + 256 * f);
+            }
+            const int32_t seen = there ? limit - (kb + 16 * h) : 0;  // of the lane's 16 keys, those that its query sees
+            entries(kb + kWaves * kSpan);
+            asm volatile("" ::: "memory");
+            i32x4 s[4];
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    s[g][t] = i32x4{0, 0, 0, 0};
+            for (int t = 0; t < 4; ++t) {
+                s[t] = i32x4{0, 0, 0, 0};
 #pragma unroll
-                    for (int n = 0; n < N; ++n)
-                        s[g][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(kr[g][t][n], q[n], s[g][t], 0, 0, 0);
-                }
+                for (int n = 0; n < N; ++n) s[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(kr[t][n], q[n], s[t], 0, 0, 0);
+            }
             int32_t top = kNone;
-#pragma unroll
-            for (int g = 0; g < KG; ++g)
+            const bool full = __all(seen >= 16);
+            if (!full) {
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if (4 * t + e >= seen[g]) s[g][t][e] = kNone;
-                        top = max(top, s[g][t][e]);
-                    }
+                    for (int e = 0; e < 4; ++e)
+                        if (4 * t + e >= seen) s[t][e] = kNone;
+            }
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) top = max(top, s[t][e]);
             top = quad_max(top);
             uint32_t sum = 0;
-            i32x4 d0[KG], d1[KG], d2[KG];
-#pragma unroll
-            for (int g = 0; g < KG; ++g)
+            i32x4 d0, d1, d2;
+            const auto weights = [&](auto masked) __attribute__((always_inline)) {
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
                     uint32_t w[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float p = __builtin_amdgcn_exp2f((float)(s[g][t][e] - top) * a.c2);
-                        w[e] = __float_as_uint(fmaf(4 * t + e < seen[g] ? p : 0.0f, kLargest, kDigits));
-                        sum += w[e] - kDigitsBits;
+                        float p = __builtin_amdgcn_exp2f((float)(s[t][e] - top) * a.c2);
+                        if (masked && 4 * t + e >= seen) p = 0.0f;  // (with a c2 of 0 too)
+                        w[e] = __float_as_uint(fmaf(p, kLargest, kDigits));
+                        sum += w[e];
                     }
                     const uint32_t low01 = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u);
                     const uint32_t low23 = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u);
                     const uint32_t top01 = __builtin_amdgcn_perm(w[1], w[0], 0x0c0c0602u);
                     const uint32_t top23 = __builtin_amdgcn_perm(w[3], w[2], 0x0c0c0602u);
-                    d0[g][t] = (int)(__builtin_amdgcn_perm(low23, low01, 0x05040100u) ^ 0x80808080u);
-                    d1[g][t] = (int)(__builtin_amdgcn_perm(low23, low01, 0x07060302u) ^ 0x80808080u);
-                    d2[g][t] = (int)__builtin_amdgcn_perm(top23, top01, 0x05040100u);
+                    d0[t] = (int)(__builtin_amdgcn_perm(low23, low01, 0x05040100u) ^ 0x80808080u);
+                    d1[t] = (int)(__builtin_amdgcn_perm(low23, low01, 0x07060302u) ^ 0x80808080u);
+                    d2[t] = (int)__builtin_amdgcn_perm(top23, top01, 0x05040100u);
                 }
+                sum -= 16 * kDigitsBits;  // (of 2^32: the sum itself is below)
+            };
+            if (full)
+                weights(std::false_type{});
+            else
+                weights(std::true_type{});
             const int32_t now = max(m, top);
             const float fo = __builtin_amdgcn_exp2f((float)(m - now) * a.c2);
             const float fb = __builtin_amdgcn_exp2f((float)(top - now) * a.c2);
             m = now;
             l = l * fo + fb * (float)sum;
+            // (two tiles of features at a time: all at once, their sums would take 12 F registers)
 #pragma unroll
-            for (int f = 0; f < F; ++f) {
-                i32x4 c0 = {0, 0, 0, 0}, c1 = {0, 0, 0, 0}, c2 = {0, 0, 0, 0};
+            for (int f0 = 0; f0 < F; f0 += FB) {
+                i32x4 c0[FB], c1[FB], c2[FB];
 #pragma unroll
-                for (int g = 0; g < KG; ++g) {
-                    c0 = __builtin_amdgcn_mfma_i32_16x16x64_i8(vr[g][f], d0[g], c0, 0, 0, 0);
-                    c1 = __builtin_amdgcn_mfma_i32_16x16x64_i8(vr[g][f], d1[g], c1, 0, 0, 0);
-                    c2 = __builtin_amdgcn_mfma_i32_16x16x64_i8(vr[g][f], d2[g], c2, 0, 0, 0);
+                for (int j = 0; j < FB; ++j) {
+                    if (f0 + j >= F) continue;
+                    const i32x4 none = {0, 0, 0, 0};
+                    c0[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vr[f0 + j], d0, none, 0, 0, 0);
+                    c1[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vr[f0 + j], d1, none, 0, 0, 0);
+                    c2[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vr[f0 + j], d2, none, 0, 0, 0);
                 }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float v = fmaf((float)c2[e], 65536.0f, (float)(c1[e] * 256 + c0[e]));
-                    o[f][e] = o[f][e] * fo + v * fb;
+                for (int j = 0; j < FB; ++j) {
+                    if (f0 + j >= F) continue;
+                    f32x4 &to = o[f0 + j];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float v = fmaf((float)c2[j][e], 65536.0f, (float)(c1[j][e] * 256 + c0[j][e]));
+                        to[e] = to[e] * fo + v * fb;
+                    }
+                    asm volatile("" : "+v"(to));
                 }
+                if (f0 + FB < F) asm volatile("" : "+v"(vr[f0 + FB]));  // (the next ones' products after this)
             }
         }
         // the waves' m, l and O together
@@ -381,7 +407,8 @@ __global__ __launch_bounds__(64 * kWaves) void cache_split_kernel(const CacheArg
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) sum += ls[w][r] * __builtin_amdgcn_exp2f((float)(ms[w][r] - mm) * a.c2);
         __syncthreads();
-        float *rec = whole ? nullptr : a.work + ((int64_t)(sh * a.tiles + tile) * a.splits + split) * record(HD);
+        float *rec = whole ? nullptr
+                           : a.work + ((((int64_t)seq * a.n_kv + kv) * a.tiles + tile) * a.splits + split) * record(HD);
         if (rec && wave == 0 && h == 0) {
             reinterpret_cast<int32_t *>(rec)[r] = mm;
             rec[16 + r] = sum;
@@ -404,14 +431,15 @@ __global__ __launch_bounds__(64 * kWaves) void cache_split_kernel(const CacheArg
     }
 }
 
-// The parts of a tile of 16 queries together. One wave a query: a lane 4 features.
+// The parts of a query together: a thread takes 4 features of every `groups`-th part, and a query's threads meet in LDS.
 __global__ __launch_bounds__(256) void cache_join_kernel(const CacheArgs a)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint32_t item = blockIdx.x;
-    const int32_t tile = (int32_t)(item % (uint32_t)a.tiles);
-    const uint32_t sh = item / (uint32_t)a.tiles;
-    const int32_t kv = (int32_t)(sh % (uint32_t)a.n_kv), seq = (int32_t)(sh / (uint32_t)a.n_kv);
+    __shared__ __attribute__((aligned(16))) float sums[256][4];
+    __shared__ float ls[256];
+    __shared__ int32_t ms[256];
+    const int tid = threadIdx.x;
+    const int32_t seq = a.seq0 + blockIdx.y;
+    const int32_t kv = a.tiles == 1 ? blockIdx.x : blockIdx.x / (uint32_t)a.tiles, tile = blockIdx.x - kv * a.tiles;
     const Tokens tk = tokens_of(a.seq_start, seq, a.m);
     const int64_t rows = (int64_t)tk.n * a.group;
     const int32_t len = max(a.kv_len[seq], 0);
@@ -419,25 +447,55 @@ __global__ __launch_bounds__(256) void cache_join_kernel(const CacheArgs a)
     const int64_t last_row = min((int64_t)tile * 16 + 15, rows - 1);
     const int32_t most = a.causal ? min(len - tk.n + (int32_t)(last_row / a.group) + 1, cached) : cached;
     const int32_t n = min(a.splits, max(1, (most + a.split_keys - 1) / a.split_keys));
-    const float *rec = a.work + (int64_t)item * a.splits * record(a.hd);
-    for (int r = wave; r < 16; r += 4) {
+    const float *rec = a.work + (((int64_t)seq * a.n_kv + kv) * a.tiles + tile) * a.splits * record(a.hd);
+    const int quads = a.hd / 4, groups = 256 / quads, group = tid / quads, c = tid % quads * 4;
+    // (as many rows as a tile was said to have; a sequence with more tokens than that has more)
+    for (int r = blockIdx.z; r < 16 && (int64_t)tile * 16 + r < rows; r += a.join_rows) {
         const int64_t row = (int64_t)tile * 16 + r;
-        if (row >= rows) return;
-        int32_t mm = kNone;
-        for (int s = lane; s < n; s += 64) mm = max(mm, reinterpret_cast<const int32_t *>(rec + s * record(a.hd))[r]);
-#pragma unroll
-        for (int d = 32; d; d >>= 1) mm = max(mm, __shfl_xor(mm, d));
+        int32_t m = kNone;
         float l = 0.0f;
         f32x4 o = {0, 0, 0, 0};
-        const int c = 4 * lane;
-        for (int s = 0; s < n; ++s) {
-            const float *p = rec + s * record(a.hd);
-            const float f = __builtin_amdgcn_exp2f((float)(reinterpret_cast<const int32_t *>(p)[r] - mm) * a.c2);
-            l += p[16 + r] * f;
-            if (c < a.hd) o += *reinterpret_cast<const f32x4 *>(p + 32 + r * a.hd + c) * f;
+        for (int s0 = group; s0 < n && group < groups; s0 += 4 * groups) {
+            int32_t mp[4];
+            float lp[4];
+            f32x4 op[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int s = s0 + j * groups;
+                const float *p = rec + (int64_t)min(s, n - 1) * record(a.hd);
+                mp[j] = s < n ? reinterpret_cast<const int32_t *>(p)[r] : kNone;
+                lp[j] = s < n ? p[16 + r] : 0.0f;
+                op[j] = *reinterpret_cast<const f32x4 *>(p + 32 + r * a.hd + c);
+            }
+            const int32_t now = max(max(max(mp[0], mp[1]), max(mp[2], mp[3])), m);
+            const float f = __builtin_amdgcn_exp2f((float)(m - now) * a.c2);
+            l *= f;
+            o *= f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float g = s0 + j * groups < n ? __builtin_amdgcn_exp2f((float)(mp[j] - now) * a.c2) : 0.0f;
+                l += lp[j] * g;
+                o += op[j] * g;
+            }
+            m = now;
         }
-        if (c < a.hd)
+        ms[tid] = m;
+        ls[tid] = l;
+        *reinterpret_cast<f32x4 *>(sums[tid]) = o;
+        __syncthreads();
+        if (group == 0) {
+            int32_t mm = m;
+            for (int g = 1; g < groups; ++g) mm = max(mm, ms[g * quads + tid]);
+            l = 0.0f;
+            o = f32x4{0, 0, 0, 0};
+            for (int g = 0; g < groups; ++g) {
+                const float f = __builtin_amdgcn_exp2f((float)(ms[g * quads + tid] - mm) * a.c2);
+                l += ls[g * quads + tid] * f;
+                o += *reinterpret_cast<const f32x4 *>(sums[g * quads + tid]) * f;
+            }
             store_row(a, (int64_t)tk.first + (int32_t)(row / a.group), kv * a.group + (int32_t)(row % a.group), c, o, l);
+        }
+        __syncthreads();
     }
 }
 
@@ -452,7 +510,7 @@ Plan plan_of(const sl_cache_attention_args &a)
     const double all = (double)a.n_seq * a.n_kv_heads * (double)p.tiles;  // (a product of whole numbers may not fit)
     if (all >= 512) return p;
     const int64_t items = (int64_t)all;
-    const int64_t want = std::min<int64_t>((512 + items - 1) / items, ((int64_t)a.max_len + 255) / 256);
+    const int64_t want = std::min<int64_t>((512 + items - 1) / items, ((int64_t)a.max_len + 511) / 512);
     if (want > 1) {
         p.split_keys = (int32_t)((((int64_t)a.max_len + want - 1) / want + 255) / 256 * 256);
         p.splits = (int32_t)(((int64_t)a.max_len + p.split_keys - 1) / p.split_keys);
@@ -461,9 +519,9 @@ Plan plan_of(const sl_cache_attention_args &a)
 }
 
 template <int F>
-sl_status launch_split(const CacheArgs &a, hipStream_t s)
+sl_status launch_split(const CacheArgs &a, dim3 grid, hipStream_t s)
 {
-    hipLaunchKernelGGL((cache_split_kernel<F, 2>), dim3((uint32_t)a.n_items), dim3(64 * kWaves), 0, s, a);
+    hipLaunchKernelGGL((cache_split_kernel<F>), grid, dim3(64 * kWaves), 0, s, a);
     HIP_TRY(hipGetLastError());
     return SL_OK;
 }
@@ -526,7 +584,7 @@ sl_status launch_cache_attention(const sl_cache_attention_args &args, void *stre
     a.work = static_cast<float *>(args.workspace);
     a.m = args.m_tokens;
     const Plan p = plan_of(args);
-    if ((double)args.n_seq * args.n_kv_heads * (double)p.tiles * p.splits > 0x7fffffff / (64 * kWaves)) {
+    if ((double)args.n_kv_heads * (double)p.tiles > 0x7fffffff / (64 * kWaves)) {
         set_error("too many work items for one launch");
         return SL_ERR_UNSUPPORTED;
     }
@@ -549,25 +607,33 @@ sl_status launch_cache_attention(const sl_cache_attention_args &args, void *stre
     a.c2 = (float)((double)args.q_scale * args.k_scale * args.softmax_scale * 1.4426950408889634);
     a.vs = args.v_scale;
     a.inv_so = a.y_f32 ? 1.0f : 1.0f / args.out_scale;
-    a.n_items = (int64_t)a.n_seq * a.n_kv * a.tiles * a.splits;
+    a.inv_group = 1.0f / a.group;
+    a.join_rows = (int32_t)std::min<int64_t>(16, (int64_t)args.max_new * a.group);
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    sl_status st;
-    switch (a.hd / 16) {
-    case 1: st = launch_split<1>(a, s); break;
-    case 2: st = launch_split<2>(a, s); break;
-    case 3: st = launch_split<3>(a, s); break;
-    case 4: st = launch_split<4>(a, s); break;
-    case 5: st = launch_split<5>(a, s); break;
-    case 6: st = launch_split<6>(a, s); break;
-    case 7: st = launch_split<7>(a, s); break;
-    default: st = launch_split<8>(a, s); break;
+    constexpr int32_t kMostGrid = 65535;  // workgroups of a launch in its second and third dimension
+    for (int64_t s0 = 0; s0 < a.n_seq; s0 += kMostGrid) {
+        a.seq0 = (int32_t)s0;
+        dim3 grid((uint32_t)(a.n_kv * a.tiles), (uint32_t)std::min(a.n_seq - a.seq0, kMostGrid), (uint32_t)a.splits);
+        sl_status st;
+        switch (a.hd / 16) {
+        case 1: st = launch_split<1>(a, grid, s); break;
+        case 2: st = launch_split<2>(a, grid, s); break;
+        case 3: st = launch_split<3>(a, grid, s); break;
+        case 4: st = launch_split<4>(a, grid, s); break;
+        case 5: st = launch_split<5>(a, grid, s); break;
+        case 6: st = launch_split<6>(a, grid, s); break;
+        case 7: st = launch_split<7>(a, grid, s); break;
+        default: st = launch_split<8>(a, grid, s); break;
+        }
+        if (st != SL_OK) return st;
+        if (a.splits > 1) {
+            grid.z = (uint32_t)a.join_rows;
+            hipLaunchKernelGGL(cache_join_kernel, grid, dim3(256), 0, s, a);
+            HIP_TRY(hipGetLastError());
+        }
     }
-    if (st == SL_OK && a.splits > 1) {
-        hipLaunchKernelGGL(cache_join_kernel, dim3((uint32_t)(a.n_items / a.splits)), dim3(256), 0, s, a);
-        HIP_TRY(hipGetLastError());
-    }
-    if (st == SL_OK) set_last_path("cache split %d,%d", a.hd, a.splits);
-    return st;
+    set_last_path("cache split %d,%d", a.hd, a.splits);
+    return SL_OK;
 }
 
 }  // namespace sl
