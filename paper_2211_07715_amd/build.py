@@ -25,7 +25,8 @@ ARCH = "gfx950"
 DEVICE_FLAGS = ["-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 HOST_SOURCES = ["api.cpp", "pack.cpp", "gelu_table.cpp", "encoder_api.cpp"]
 HIP_SOURCES = ["kernels.hip", "kernels_direct.hip", "kernels_panel.hip", "kernels_split.hip", "kernels_tile.hip",
-               "kernels_norm.hip", "kernels_attention.hip", "kernels_cache.hip"]
+               "kernels_norm.hip", "kernels_attention.hip", "kernels_cache.hip",
+               "kernels_cache_prompt.hip"]
 # the benchmark's measurement probes (copy bandwidth, matrix-instruction
 # throughput): a library of their own, not linked into the layer's
 PROBE_SOURCES = ["probe.hip"]

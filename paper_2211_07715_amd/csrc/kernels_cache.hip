@@ -5,31 +5,12 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "cache_device.h"
 #include "encoder.h"
-#include "sl_device.h"
 
 namespace sl {
 
 namespace {
-
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-
-// tokens first .. first + n - 1 of a call that belong to a sequence
-struct Tokens {
-    int32_t first, n;
-};
-__device__ __forceinline__ Tokens tokens_of(const int32_t *seq_start, int32_t s, int64_t m)
-{
-    const int32_t m32 = (int32_t)m;
-    const int32_t b = min(max(seq_start[s], 0), m32);
-    return {b, min(max(seq_start[s + 1], b), m32) - b};
-}
-
-// byte offset of feature c of token t
-__device__ __forceinline__ int64_t at(int64_t t, int32_t c, int32_t cols, int32_t cb)
-{
-    return cb ? t16x32_offset(t, c, cb) : t * cols + c;
-}
 
 // --- cache_append --------------------------------------------------------------
 
@@ -178,17 +159,6 @@ __global__ __launch_bounds__(256) void cache_append_kernel(const AppendArgs p)
 
 constexpr int kWaves = 4;  // of a workgroup, which share its keys
 constexpr int kSpan = 64;  // keys that a wave takes at a time
-
-struct CacheArgs {
-    const int8_t *q, *cache;
-    const int32_t *seq_start, *kv_len, *page_table;
-    void *y;
-    float *work;
-    int64_t m;
-    int32_t n_seq, tiles, splits, split_keys;
-    int32_t n_heads, n_kv, group, hd, q_cols, q_cb, y_cb, shift, max_pages, n_pages, causal, y_f32, join_rows, seq0;
-    float c2, vs, inv_so, inv_group;
-};
 
 // floats of a part's record in the workspace: 16 queries' m, l and O
 __host__ __device__ constexpr int64_t record(int hd) { return 16 * (int64_t)(hd + 2); }
@@ -502,11 +472,15 @@ __global__ __launch_bounds__(256) void cache_join_kernel(const CacheArgs a)
 struct Plan {
     int64_t tiles;
     int32_t splits, split_keys;
+    bool prompt;
 };
+constexpr int32_t kMostRows = 32;
 Plan plan_of(const sl_cache_attention_args &a)
 {
     const int32_t group = a.n_heads / a.n_kv_heads;
-    Plan p{((int64_t)a.max_new * group + 15) / 16, 1, 0};
+    Plan p{((int64_t)a.max_new * group + 15) / 16, 1, 0, false};
+    p.prompt = (int64_t)a.max_new * group > kMostRows;
+    if (p.prompt) return p;
     const double all = (double)a.n_seq * a.n_kv_heads * (double)p.tiles;  // (a product of whole numbers may not fit)
     if (all >= 512) return p;
     const int64_t items = (int64_t)all;
@@ -584,7 +558,7 @@ sl_status launch_cache_attention(const sl_cache_attention_args &args, void *stre
     a.work = static_cast<float *>(args.workspace);
     a.m = args.m_tokens;
     const Plan p = plan_of(args);
-    if ((double)args.n_kv_heads * (double)p.tiles > 0x7fffffff / (64 * kWaves)) {
+    if (!p.prompt && (double)args.n_kv_heads * (double)p.tiles > 0x7fffffff / (64 * kWaves)) {
         set_error("too many work items for one launch");
         return SL_ERR_UNSUPPORTED;
     }
@@ -607,6 +581,7 @@ sl_status launch_cache_attention(const sl_cache_attention_args &args, void *stre
     a.c2 = (float)((double)args.q_scale * args.k_scale * args.softmax_scale * 1.4426950408889634);
     a.vs = args.v_scale;
     a.inv_so = a.y_f32 ? 1.0f : 1.0f / args.out_scale;
+    if (p.prompt) return launch_cache_prompt(a, args, static_cast<hipStream_t>(stream));
     a.inv_group = 1.0f / a.group;
     a.join_rows = (int32_t)std::min<int64_t>(16, (int64_t)args.max_new * a.group);
     const hipStream_t s = static_cast<hipStream_t>(stream);
