@@ -24,11 +24,25 @@ struct CacheArgs {
     float *work;
     int64_t m;
     int32_t n_seq, tiles, splits, split_keys;
-    int32_t n_heads, n_kv, group, hd, q_cols, q_cb, y_cb, shift, max_pages, n_pages, causal, y_f32, join_rows, seq0;
+    int32_t n_heads, n_kv, group, hd, q_cols, q_cb, y_cb, shift, max_pages, n_pages, causal, y_f32, tile_rows, join_group, seq0, group_shift;
     float c2, k2, vs, inv_so, inv_group;
 };
 
-// cache_attention for many queries a sequence (kernels_cache_prompt.hip)
-sl_status launch_cache_prompt(CacheArgs a, const sl_cache_attention_args &args, hipStream_t s);
+// cache_attention for many queries a sequence (kernels_cache_prompt.hip): tile_rows, 64 or 128, (query, head) pairs a
+// workgroup (64 for heads to 64 features only)
+sl_status launch_cache_prompt(const CacheArgs &a, dim3 grid, hipStream_t s);
+
+// token of a (query, head) row of a key head: x / group
+__device__ __forceinline__ int64_t by_group(const CacheArgs &a, int64_t x)
+{
+    return a.group_shift >= 0 ? x >> a.group_shift : x < 0x7fffffff ? (int64_t)((uint32_t)x / (uint32_t)a.group) : x / a.group;
+}
+__device__ __forceinline__ uint32_t by_group(const CacheArgs &a, uint32_t x)
+{
+    return a.group_shift >= 0 ? x >> a.group_shift : x / (uint32_t)a.group;
+}
+
+// floats of a part's record in the workspace: m, l and O of a workgroup's rows
+__host__ __device__ constexpr int64_t record(int hd, int rows) { return rows * (int64_t)(hd + 2); }
 
 }  // namespace sl

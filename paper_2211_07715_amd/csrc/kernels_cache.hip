@@ -160,9 +160,6 @@ __global__ __launch_bounds__(256) void cache_append_kernel(const AppendArgs p)
 constexpr int kWaves = 4;  // of a workgroup, which share its keys
 constexpr int kSpan = 64;  // keys that a wave takes at a time
 
-// floats of a part's record in the workspace: 16 queries' m, l and O
-__host__ __device__ constexpr int64_t record(int hd) { return 16 * (int64_t)(hd + 2); }
-
 __device__ __forceinline__ int quad_max(int v)  // over lanes 16 and 32 apart
 {
     const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
@@ -228,7 +225,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(3))
         const bool whole = a.splits == 1 || tile >= a.tiles;  // this workgroup alone sees all keys
         if (whole && split) continue;
         // row r: token i, head of the group
-        const int32_t i0 = tile ? (int32_t)(tile * 16 / a.group) : 0, g0 = (int32_t)(tile * 16 - (int64_t)i0 * a.group) + r;
+        const int32_t i0 = tile ? (int32_t)by_group(a, tile * 16) : 0, g0 = (int32_t)(tile * 16 - (int64_t)i0 * a.group) + r;
         const bool real = tile * 16 + r < rows;
         const int32_t di = a.group >= 16 ? (g0 >= a.group ? 1 : 0) : (int32_t)(((float)g0 + 0.5f) * a.inv_group);  // (g0 < 32)
         const int32_t i = i0 + di, head = kv * a.group + (g0 - di * a.group);
@@ -378,7 +375,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(3))
         for (int w = 0; w < kWaves; ++w) sum += ls[w][r] * __builtin_amdgcn_exp2f((float)(ms[w][r] - mm) * a.c2);
         __syncthreads();
         float *rec = whole ? nullptr
-                           : a.work + ((((int64_t)seq * a.n_kv + kv) * a.tiles + tile) * a.splits + split) * record(HD);
+                           : a.work + ((((int64_t)seq * a.n_kv + kv) * a.tiles + tile) * a.splits + split) * record(HD, 16);
         if (rec && wave == 0 && h == 0) {
             reinterpret_cast<int32_t *>(rec)[r] = mm;
             rec[16 + r] = sum;
@@ -401,7 +398,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(3))
     }
 }
 
-// The parts of a query together: a thread takes 4 features of every `groups`-th part, and a query's threads meet in LDS.
+// The parts of a query together: join_group threads of 4 features each take every join_group-th part, and meet in LDS.
 __global__ __launch_bounds__(256) void cache_join_kernel(const CacheArgs a)
 {
     __shared__ __attribute__((aligned(16))) float sums[256][4];
@@ -411,31 +408,34 @@ __global__ __launch_bounds__(256) void cache_join_kernel(const CacheArgs a)
     const int32_t seq = a.seq0 + blockIdx.y;
     const int32_t kv = a.tiles == 1 ? blockIdx.x : blockIdx.x / (uint32_t)a.tiles, tile = blockIdx.x - kv * a.tiles;
     const Tokens tk = tokens_of(a.seq_start, seq, a.m);
-    const int64_t rows = (int64_t)tk.n * a.group;
+    const int64_t first_row = (int64_t)tile * a.tile_rows;
+    const int64_t rows = min((int64_t)tk.n * a.group - first_row, (int64_t)a.tile_rows);
+    if (rows <= 0) return;
     const int32_t len = max(a.kv_len[seq], 0);
     const int32_t cached = (int32_t)min((int64_t)len, (int64_t)a.max_pages << a.shift);
-    const int64_t last_row = min((int64_t)tile * 16 + 15, rows - 1);
-    const int32_t most = a.causal ? min(len - tk.n + (int32_t)(last_row / a.group) + 1, cached) : cached;
+    const int32_t most = a.causal ? min(len - tk.n + (int32_t)by_group(a, first_row + rows - 1) + 1, cached) : cached;
     const int32_t n = min(a.splits, max(1, (most + a.split_keys - 1) / a.split_keys));
-    const float *rec = a.work + (((int64_t)seq * a.n_kv + kv) * a.tiles + tile) * a.splits * record(a.hd);
-    const int quads = a.hd / 4, groups = 256 / quads, group = tid / quads, c = tid % quads * 4;
-    // (as many rows as a tile was said to have; a sequence with more tokens than that has more)
-    for (int r = blockIdx.z; r < 16 && (int64_t)tile * 16 + r < rows; r += a.join_rows) {
-        const int64_t row = (int64_t)tile * 16 + r;
+    const float *rec = a.work + (((int64_t)seq * a.n_kv + kv) * a.tiles + tile) * a.splits * record(a.hd, a.tile_rows);
+    const int quads = a.hd / 4, per = quads * a.join_group, here_rows = 256 / per;  // rows of a workgroup at a time
+    const int mine = tid / per, group = tid % per / quads, c = tid % quads * 4;
+    // (as many workgroups as a tile was said to have rows; a sequence with more tokens than that has more)
+    for (int r0 = blockIdx.z * here_rows; r0 < rows; r0 += gridDim.z * here_rows) {
+        const int r = r0 + mine;
+        const bool real = mine < here_rows && r < rows;
         int32_t m = kNone;
         float l = 0.0f;
         f32x4 o = {0, 0, 0, 0};
-        for (int s0 = group; s0 < n && group < groups; s0 += 4 * groups) {
+        for (int s0 = group; s0 < n && real; s0 += 4 * a.join_group) {
             int32_t mp[4];
             float lp[4];
             f32x4 op[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int s = s0 + j * groups;
-                const float *p = rec + (int64_t)min(s, n - 1) * record(a.hd);
+                const int s = s0 + j * a.join_group;
+                const float *p = rec + (int64_t)min(s, n - 1) * record(a.hd, a.tile_rows);
                 mp[j] = s < n ? reinterpret_cast<const int32_t *>(p)[r] : kNone;
-                lp[j] = s < n ? p[16 + r] : 0.0f;
-                op[j] = *reinterpret_cast<const f32x4 *>(p + 32 + r * a.hd + c);
+                lp[j] = s < n ? p[a.tile_rows + r] : 0.0f;
+                op[j] = *reinterpret_cast<const f32x4 *>(p + 2 * a.tile_rows + r * a.hd + c);
             }
             const int32_t now = max(max(max(mp[0], mp[1]), max(mp[2], mp[3])), m);
             const float f = __builtin_amdgcn_exp2f((float)(m - now) * a.c2);
@@ -443,48 +443,59 @@ __global__ __launch_bounds__(256) void cache_join_kernel(const CacheArgs a)
             o *= f;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float g = s0 + j * groups < n ? __builtin_amdgcn_exp2f((float)(mp[j] - now) * a.c2) : 0.0f;
+                const float g = s0 + j * a.join_group < n ? __builtin_amdgcn_exp2f((float)(mp[j] - now) * a.c2) : 0.0f;
                 l += lp[j] * g;
                 o += op[j] * g;
             }
             m = now;
         }
-        ms[tid] = m;
-        ls[tid] = l;
-        *reinterpret_cast<f32x4 *>(sums[tid]) = o;
-        __syncthreads();
-        if (group == 0) {
-            int32_t mm = m;
-            for (int g = 1; g < groups; ++g) mm = max(mm, ms[g * quads + tid]);
-            l = 0.0f;
-            o = f32x4{0, 0, 0, 0};
-            for (int g = 0; g < groups; ++g) {
-                const float f = __builtin_amdgcn_exp2f((float)(ms[g * quads + tid] - mm) * a.c2);
-                l += ls[g * quads + tid] * f;
-                o += *reinterpret_cast<const f32x4 *>(sums[g * quads + tid]) * f;
+        if (a.join_group > 1) {
+            ms[tid] = m;
+            ls[tid] = l;
+            *reinterpret_cast<f32x4 *>(sums[tid]) = o;
+            __syncthreads();
+            if (group == 0 && real) {
+                int32_t mm = m;
+                for (int g = 1; g < a.join_group; ++g) mm = max(mm, ms[tid + g * quads]);
+                l = 0.0f;
+                o = f32x4{0, 0, 0, 0};
+                for (int g = 0; g < a.join_group; ++g) {
+                    const float f = __builtin_amdgcn_exp2f((float)(ms[tid + g * quads] - mm) * a.c2);
+                    l += ls[tid + g * quads] * f;
+                    o += *reinterpret_cast<const f32x4 *>(sums[tid + g * quads]) * f;
+                }
             }
-            store_row(a, (int64_t)tk.first + (int32_t)(row / a.group), kv * a.group + (int32_t)(row % a.group), c, o, l);
+            __syncthreads();
         }
-        __syncthreads();
+        if (group == 0 && real) {
+            const int64_t row = first_row + r;
+            const int32_t i = (int32_t)by_group(a, row);
+            store_row(a, (int64_t)tk.first + i, kv * a.group + (int32_t)(row - (int64_t)i * a.group), c, o, l);
+        }
     }
 }
 
 struct Plan {
-    int64_t tiles;
-    int32_t splits, split_keys;
     bool prompt;
+    int32_t tile_rows, splits, split_keys;
+    int64_t tiles;
 };
-constexpr int32_t kMostRows = 32;
+
 Plan plan_of(const sl_cache_attention_args &a)
 {
     const int32_t group = a.n_heads / a.n_kv_heads;
-    Plan p{((int64_t)a.max_new * group + 15) / 16, 1, 0, false};
-    p.prompt = (int64_t)a.max_new * group > kMostRows;
-    if (p.prompt) return p;
-    const double all = (double)a.n_seq * a.n_kv_heads * (double)p.tiles;  // (a product of whole numbers may not fit)
-    if (all >= 512) return p;
+    const int64_t rows = (int64_t)a.max_new * group;
+    const auto items_of = [&](int32_t tile_rows) {  // (a product of whole numbers may not fit)
+        return (double)a.n_seq * a.n_kv_heads * (double)((rows + tile_rows - 1) / tile_rows);
+    };
+    Plan p{rows > 16 && items_of(16) > 384, 16, 1, 0, 0};
+    if (p.prompt) p.tile_rows = a.head_dim <= 64 && items_of(128) < 800 && a.max_len >= 256 ? 64 : 128;
+    p.tiles = (rows + p.tile_rows - 1) / p.tile_rows;
+    const double all = items_of(p.tile_rows);
+    const int32_t enough = p.prompt ? 384 : 512, least = p.prompt ? 1024 : 512;
+    if (all >= enough) return p;
     const int64_t items = (int64_t)all;
-    const int64_t want = std::min<int64_t>((512 + items - 1) / items, ((int64_t)a.max_len + 511) / 512);
+    const int64_t want = std::min<int64_t>((enough + items - 1) / items, ((int64_t)a.max_len + least - 1) / least);
     if (want > 1) {
         p.split_keys = (int32_t)((((int64_t)a.max_len + want - 1) / want + 255) / 256 * 256);
         p.splits = (int32_t)(((int64_t)a.max_len + p.split_keys - 1) / p.split_keys);
@@ -506,7 +517,7 @@ int64_t cache_attention_bytes(const sl_cache_attention_args &a)
 {
     const Plan p = plan_of(a);
     if (p.splits == 1) return 0;
-    return (int64_t)a.n_seq * a.n_kv_heads * p.tiles * p.splits * record(a.head_dim) * 4;
+    return (int64_t)a.n_seq * a.n_kv_heads * p.tiles * p.splits * record(a.head_dim, p.tile_rows) * 4;
 }
 
 sl_status launch_cache_append(const sl_cache_append_args &args, void *stream)
@@ -558,12 +569,13 @@ sl_status launch_cache_attention(const sl_cache_attention_args &args, void *stre
     a.work = static_cast<float *>(args.workspace);
     a.m = args.m_tokens;
     const Plan p = plan_of(args);
-    if (!p.prompt && (double)args.n_kv_heads * (double)p.tiles > 0x7fffffff / (64 * kWaves)) {
+    constexpr int32_t kMostGrid = 65535;  // workgroups of a launch in its second and third dimension
+    if ((double)args.n_seq * args.n_kv_heads * (double)p.tiles * p.splits > 0x7fffffff / 256) {
         set_error("too many work items for one launch");
         return SL_ERR_UNSUPPORTED;
     }
     a.n_seq = args.n_seq;
-    a.tiles = (int32_t)p.tiles;
+    a.tiles = (int32_t)(p.prompt ? std::min<int64_t>(p.tiles, kMostGrid / p.splits) : p.tiles);
     a.splits = p.splits;
     a.split_keys = p.split_keys;
     a.n_heads = args.n_heads;
@@ -581,16 +593,27 @@ sl_status launch_cache_attention(const sl_cache_attention_args &args, void *stre
     a.c2 = (float)((double)args.q_scale * args.k_scale * args.softmax_scale * 1.4426950408889634);
     a.vs = args.v_scale;
     a.inv_so = a.y_f32 ? 1.0f : 1.0f / args.out_scale;
-    if (p.prompt) return launch_cache_prompt(a, args, static_cast<hipStream_t>(stream));
     a.inv_group = 1.0f / a.group;
-    a.join_rows = (int32_t)std::min<int64_t>(16, (int64_t)args.max_new * a.group);
+    a.group_shift = (a.group & (a.group - 1)) ? -1 : __builtin_ctz(a.group);
+    a.tile_rows = p.tile_rows;
+    if (p.prompt) {
+        const Exponent e = exponent_of((double)args.q_scale * args.k_scale * args.softmax_scale);
+        a.c2 = e.c2;
+        a.k2 = e.k2;
+    }
+    // threads of a row's 4 features that share its parts, 4 and more each; and workgroups for a tile's rows
+    const int32_t quads = a.hd / 4;
+    a.join_group = std::min(256 / quads, (a.splits + 3) / 4);
+    const int32_t at_a_time = 256 / (quads * a.join_group);
+    const int32_t join_z = (int32_t)((std::min<int64_t>(a.tile_rows, (int64_t)args.max_new * a.group) + at_a_time - 1) / at_a_time);
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    constexpr int32_t kMostGrid = 65535;  // workgroups of a launch in its second and third dimension
     for (int64_t s0 = 0; s0 < a.n_seq; s0 += kMostGrid) {
         a.seq0 = (int32_t)s0;
-        dim3 grid((uint32_t)(a.n_kv * a.tiles), (uint32_t)std::min(a.n_seq - a.seq0, kMostGrid), (uint32_t)a.splits);
-        sl_status st;
-        switch (a.hd / 16) {
+        const uint32_t seqs = (uint32_t)std::min(a.n_seq - a.seq0, kMostGrid);
+        const dim3 grid((uint32_t)(a.n_kv * a.tiles), seqs, (uint32_t)a.splits);
+        sl_status st = SL_OK;
+        switch (p.prompt ? 0 : a.hd / 16) {
+        case 0: st = launch_cache_prompt(a, dim3((uint32_t)a.n_kv, seqs, (uint32_t)(a.tiles * a.splits)), s); break;
         case 1: st = launch_split<1>(a, grid, s); break;
         case 2: st = launch_split<2>(a, grid, s); break;
         case 3: st = launch_split<3>(a, grid, s); break;
@@ -602,12 +625,11 @@ sl_status launch_cache_attention(const sl_cache_attention_args &args, void *stre
         }
         if (st != SL_OK) return st;
         if (a.splits > 1) {
-            grid.z = (uint32_t)a.join_rows;
-            hipLaunchKernelGGL(cache_join_kernel, grid, dim3(256), 0, s, a);
+            hipLaunchKernelGGL(cache_join_kernel, dim3(grid.x, seqs, (uint32_t)join_z), dim3(256), 0, s, a);
             HIP_TRY(hipGetLastError());
         }
     }
-    set_last_path("cache split %d,%d", a.hd, a.splits);
+    set_last_path("cache %s %d,%d", p.prompt ? "prompt" : "split", a.hd, a.splits);
     return SL_OK;
 }
 

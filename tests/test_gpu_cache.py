@@ -292,6 +292,22 @@ def test_attention_many_sequences(hip):
     run_attend(hip, rng, Batch(hip, rng, [1] * 700, lens, 16, 1, 16), 1)
 
 
+@pytest.mark.parametrize("news,lens", [([40], [5000]), ([130, 3, 1], [3000, 2050, 1]), ([33, 129], [2049, 140])])
+@pytest.mark.parametrize("nh,nkv,hd", [(2, 2, 64), (4, 1, 128), (3, 1, 16)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_attention_of_many_queries_in_parts(hip, news, lens, nh, nkv, hd, causal):
+    rng = np.random.default_rng(news[0] + hd)
+    run_attend(hip, rng, Batch(hip, rng, news, lens, 16, nkv, hd, gap=1, holes=hd == 16), nh, causal=causal)
+
+
+@pytest.mark.parametrize("new", [2, 50])
+def test_attention_in_parts_of_more_than_said(hip, new):
+    rng = np.random.default_rng(19)
+    b = Batch(hip, rng, [new + 30, new, 140], [6000, 700, 2500], 16, 1, 64)
+    b.most_new, b.longest = new, 2100
+    run_attend(hip, rng, b, 2)
+
+
 def test_attention_long(hip):
     rng = np.random.default_rng(18)
     run_attend(hip, rng, Batch(hip, rng, [1, 2], [40000, 9999], 64, 1, 64), 8)
