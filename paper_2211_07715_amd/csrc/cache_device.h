@@ -9,12 +9,17 @@ namespace sl {
 struct Tokens {
     int32_t first, n;
 };
-__device__ __forceinline__ Tokens tokens_of(const int32_t *seq_start, int32_t s, int64_t m)
+__device__ __forceinline__ Tokens tokens_between(int32_t start, int32_t end, int64_t m)
 {
     const int32_t m32 = (int32_t)m;
-    const int32_t b = min(max(seq_start[s], 0), m32);
-    return {b, min(max(seq_start[s + 1], b), m32) - b};
+    const int32_t b = min(max(start, 0), m32);
+    return {b, min(max(end, b), m32) - b};
 }
+__device__ __forceinline__ Tokens tokens_of(const int32_t *seq_start, int32_t s, int64_t m)
+{
+    return tokens_between(seq_start[s], seq_start[s + 1], m);
+}
+typedef const __attribute__((address_space(4))) int32_t *ScalarTable;  // read through the scalar cache
 
 // cache_attention's arguments as its kernels take them
 struct CacheArgs {

@@ -214,9 +214,12 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(3))
         pv = table[min((kb + 16 * h) >> a.shift, last_entry)];
     };
     if (a.max_pages) entries(split * a.split_keys + wave * kSpan);  // (on their way with the lengths)
-    const Tokens tk = tokens_of(a.seq_start, seq, a.m);
+    int32_t b0 = ((ScalarTable)(uintptr_t)a.seq_start)[seq], b1 = ((ScalarTable)(uintptr_t)a.seq_start)[seq + 1];
+    int32_t len = ((ScalarTable)(uintptr_t)a.kv_len)[seq];
+    asm volatile("" : "+s"(b0), "+s"(b1), "+s"(len));  // (here they are all waited for, instead of one after the other)
+    const Tokens tk = tokens_between(b0, b1, a.m);
     const int64_t rows = (int64_t)tk.n * a.group;
-    const int32_t len = max(a.kv_len[seq], 0);
+    len = max(len, 0);
     const int32_t cached = (int32_t)min((int64_t)len, (int64_t)a.max_pages << a.shift);
     const int64_t head_bytes = (int64_t)HD << a.shift, page_bytes = 2 * a.n_kv * head_bytes;
     const int8_t *keys = a.cache + kv * head_bytes, *values = keys + a.n_kv * head_bytes;
@@ -489,7 +492,11 @@ Plan plan_of(const sl_cache_attention_args &a)
         return (double)a.n_seq * a.n_kv_heads * (double)((rows + tile_rows - 1) / tile_rows);
     };
     Plan p{rows > 16 && items_of(16) > 384, 16, 1, 0, 0};
-    if (p.prompt) p.tile_rows = a.head_dim <= 64 && items_of(128) < 800 && a.max_len >= 256 ? 64 : 128;
+    if (p.prompt) {
+        // (m_tokens bounds what sequences of different lengths have together: half a tile more each)
+        const double real = (double)a.n_kv_heads * ((double)a.m_tokens * group / 128 + 0.5 * a.n_seq);
+        p.tile_rows = a.head_dim <= 64 && std::min(items_of(128), real) < 512 ? 64 : 128;
+    }
     p.tiles = (rows + p.tile_rows - 1) / p.tile_rows;
     const double all = items_of(p.tile_rows);
     const int32_t enough = p.prompt ? 384 : 512, least = p.prompt ? 1024 : 512;

@@ -22,8 +22,6 @@ namespace sl {
 
 namespace {
 
-typedef const __attribute__((address_space(4))) int32_t *ScalarTable;  // read through the scalar cache
-
 // N: 32-feature tiles of a head. A wave has 32 queries; RW waves share a chunk of
 // keys, and the 4 / RW sets of them in a workgroup have the same queries and take
 // turns at the chunks, until their m, l and O meet in LDS at the end.
@@ -46,24 +44,35 @@ void cache_prompt_kernel(const CacheArgs a)
     const int32_t kv = blockIdx.x, seq = a.seq0 + blockIdx.y;
     const int32_t from_last = a.splits == 1 ? blockIdx.z : blockIdx.z / (uint32_t)a.splits;
     const int32_t tile0 = a.tiles - 1 - from_last, split = blockIdx.z - from_last * a.splits;
-    const ScalarTable table = (ScalarTable)(uintptr_t)(a.page_table + (int64_t)seq * a.max_pages);
-    // pages of a chunk: of the wave's own groups, and which of the four are none
-    int32_t own[G] = {};
-    uint32_t none = 0;
-    const auto entries = [&](int32_t c) __attribute__((always_inline)) {
+    // (without pages nothing is taken from it; the read has to be somewhere)
+    const int32_t *row_of_table = a.max_pages ? a.page_table + (int64_t)seq * a.max_pages : a.kv_len;
+    const ScalarTable table = (ScalarTable)(uintptr_t)row_of_table;
+    const int32_t last_entry = max(a.max_pages - 1, 0);
+    // numbers of a chunk's four pages: asked for (all at once, well ahead), and then taken: the wave's own groups', and
+    // which of the four are none
+    int32_t asked[4], own[G];
+    uint32_t none;
+    const auto ask = [&](int32_t c) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) asked[j] = table[min((kChunk * c + 16 * j) >> a.shift, last_entry)];
+    };
+    const auto take = [&]() __attribute__((always_inline)) {
         none = 0;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int32_t e = table[min((kChunk * c + 16 * j) >> a.shift, a.max_pages - 1)];
-            const bool there = (uint32_t)e < (uint32_t)a.n_pages;
+            const bool there = (uint32_t)asked[j] < (uint32_t)a.n_pages;
             none |= there ? 0u : 1u << j;
-            if (j / G == wave) own[j % G] = there ? e : 0;
+            if (j / G == wave) own[j % G] = there ? asked[j] : 0;
         }
     };
-    if (a.max_pages) entries(split * (a.split_keys / kChunk) + part);  // (on their way with the lengths)
-    const Tokens tk = tokens_of(a.seq_start, seq, a.m);
+    ask(split * (a.split_keys / kChunk) + part);
+    int32_t b0 = ((ScalarTable)(uintptr_t)a.seq_start)[seq], b1 = ((ScalarTable)(uintptr_t)a.seq_start)[seq + 1];
+    int32_t len = ((ScalarTable)(uintptr_t)a.kv_len)[seq];
+    // (here they are all waited for, instead of one after the other)
+    asm volatile("" : "+s"(asked[0]), "+s"(asked[1]), "+s"(asked[2]), "+s"(asked[3]), "+s"(b0), "+s"(b1), "+s"(len));
+    const Tokens tk = tokens_between(b0, b1, a.m);
+    len = max(len, 0);
     const int64_t rows = (int64_t)tk.n * a.group;
-    const int32_t len = max(a.kv_len[seq], 0);
     const int32_t cached = (int32_t)min((int64_t)len, (int64_t)a.max_pages << a.shift);
     const int64_t head_bytes = (int64_t)a.hd << a.shift, page_bytes = 2 * a.n_kv * head_bytes;
     const int8_t *keys = a.cache + kv * head_bytes, *values = keys + a.n_kv * head_bytes;
@@ -223,16 +232,18 @@ void cache_prompt_kernel(const CacheArgs a)
             for (int w = 0; w < 4; ++w) {  // 16 keys
 #pragma unroll
                 for (int j = 0; j < 8; j += 2) {
-                    float e[2], hi[2];
+                    float e[2];
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
                         const int i = 8 * (w & 1) + j + r;
                         e[r] = __builtin_amdgcn_exp2f(fmaf(__int_as_float(s[w / 2][i]), a.c2, a.k2));
                         sum[2 * (w & 1) + r] += e[r];
-                        hi[r] = __uint_as_float(__float_as_uint(e[r]) & 0xffffe000u);
                     }
-                    const f16x2 h = __builtin_convertvector((f32x2{hi[0], hi[1]}), f16x2);
-                    const f16x2 l2 = __builtin_convertvector((f32x2{e[0] - hi[0], e[1] - hi[1]}), f16x2);
+                    const f16x2 h = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(e[0], e[1]));
+                    float rest[2];
+                    asm("v_fma_mix_f32 %0, -%1, 1.0, %2 op_sel_hi:[1,0,0]" : "=v"(rest[0]) : "v"(h), "v"(e[0]));
+                    asm("v_fma_mix_f32 %0, -%1, 1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(rest[1]) : "v"(h), "v"(e[1]));
+                    const f16x2 l2 = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(rest[0], rest[1]));
                     p[w][j] = h[0];
                     p[w][j + 1] = h[1];
                     p2[w][j] = l2[0];
@@ -256,16 +267,21 @@ void cache_prompt_kernel(const CacheArgs a)
         int32_t c = c0 + part, buf = 0;
         uint32_t gone = 0;  // which of the chunk's pages are none
         if (c < n_chunks) {
-            if (tile != tile0) entries(c);
+            if (tile != tile0) ask(c);
+            take();
             gone = none;
             load(c, lds);
-            entries(c + KW);
+            ask(c + KW);
             stage(lds);
+            take();
         }
         __syncthreads();
         // every chunk: the next one's loads, this one's work, then the next one goes to LDS
         const auto bring = [&]() __attribute__((always_inline)) {
-            if (c + KW < n_chunks) load(c + KW, lds + (buf ^ BUF));
+            if (c + KW < n_chunks) {
+                load(c + KW, lds + (buf ^ BUF));
+                ask(c + 2 * KW);
+            }
         };
         const auto advance = [&]() __attribute__((always_inline)) {
             buf ^= BUF;
@@ -273,7 +289,7 @@ void cache_prompt_kernel(const CacheArgs a)
             gone = none;
             if (c < n_chunks) {
                 stage(lds + buf);
-                entries(c + KW);
+                take();
             }
             __syncthreads();
         };
