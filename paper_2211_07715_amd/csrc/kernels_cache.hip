@@ -17,8 +17,10 @@ namespace {
 struct AppendArgs {
     sl_cache_append_args a;
     int32_t cols, x_cb, q_cb, shift;  // 1 << shift: tokens of a page
-    int32_t quads, parts;             // workgroups along a sequence's tokens, and along its features
-    float fq, fk, fv;                 // from x's unit to the codes'
+    int32_t qk_columns, columns, per;  // a thread each: of queries and keys, and of all; `per` a workgroup
+    int32_t seq0;
+    float fq, fk, fv;  // from x's unit to the codes'
+    float inv_qk, inv_value;  // 1 / columns of a head
 };
 
 __device__ __forceinline__ f32x4 codes_to_float(uint32_t w)
@@ -26,130 +28,295 @@ __device__ __forceinline__ f32x4 codes_to_float(uint32_t w)
     return f32x4{(float)(int8_t)w, (float)(int8_t)(w >> 8), (float)(int8_t)(w >> 16), (float)(int8_t)(w >> 24)};
 }
 
+// Codes of 4 values. 1.5 * 2^23 more than value * f is rounded to a whole number, whose
+// low byte is the code once it is within 127 of that.
+__device__ __forceinline__ uint32_t code_bits(float v, float f)
+{
+    return __float_as_uint(__builtin_amdgcn_fmed3f(fmaf(v, f, kMagicF), kMagicF - 127.0f, kMagicF + 127.0f));
+}
 __device__ __forceinline__ uint32_t codes_of(f32x4 v, float f)
 {
-    return pack_bytes(requant_bits(v[0], f), requant_bits(v[1], f), requant_bits(v[2], f), requant_bits(v[3], f));
+    return pack_bytes(code_bits(v[0], f), code_bits(v[1], f), code_bits(v[2], f), code_bits(v[3], f));
 }
 
-// One workgroup: up to 4 consecutive slots (one word of a feature's values in the
-// cache) of one sequence, and a share of the features. VEC: rope_dim is a multiple
-// of 8, so that 4 features of a pair's halves lie together.
+// What a thread does: a column, which is 8 features of a query or key head (VEC:
+// rope_dim is a multiple of 8, so that 4 features of both halves of pairs lie
+// together; else 2 features), or 4 features of a value head.
 template <bool F32, bool VEC>
-__global__ __launch_bounds__(256) void cache_append_kernel(const AppendArgs p)
-{
-    __shared__ __attribute__((aligned(16))) float cs[4][64], sn[4][64];
-    const sl_cache_append_args &a = p.a;
-    const int tid = threadIdx.x;
-    const int32_t part = (int32_t)(blockIdx.x % (uint32_t)p.parts);
-    const int32_t quad = (int32_t)(blockIdx.x / (uint32_t)p.parts % (uint32_t)p.quads);
-    const int32_t seq = (int32_t)(blockIdx.x / (uint32_t)p.parts / (uint32_t)p.quads);
-    const Tokens tk = tokens_of(a.seq_start, seq, a.m_tokens);
-    if (tk.n == 0) return;
-    const int32_t hd = a.head_dim, nh = a.n_heads, nkv = a.n_kv_heads, half = a.rope_kind ? a.rope_dim / 2 : 0;
-    const int32_t len = max(a.kv_len[seq], 0);
-    const int64_t p0 = (int64_t)len - tk.n;  // the first token's slot
-    const float *xf = static_cast<const float *>(a.x);
-    const int8_t *xc = static_cast<const int8_t *>(a.x);
-    const auto load4 = [&](int64_t t, int32_t c) {
+struct Column {
+    static constexpr int U = VEC ? 8 : 2;
+    const AppendArgs &p;
+    bool mine, is_value, turned, split;
+    int32_t head, w0, c0;     // first angle, first feature
+    uint32_t x0, x1, q0, q1;  // bytes of both parts from a token's first in x and q,
+    uint32_t k0, k1;          // and from a slot's of head 0 in a page's keys
+    float f;
+    // A token's place is the same for all lanes, a column's the same for all tokens: addresses are sums of the two.
+    __device__ __forceinline__ static uint32_t offset(int32_t c, int32_t cb, int32_t size)
+    {
+        return cb ? (uint32_t)(c >> 5) * 512 + (c & 31) : (uint32_t)c * size;
+    }
+    __device__ __forceinline__ static int64_t token(int64_t t, int32_t cols, int32_t cb, int32_t size)
+    {
+        return cb ? (t >> 4) * cb * 512 + (t & 15) * 32 : t * cols * size;
+    }
+    __device__ __forceinline__ Column(const AppendArgs &p_, int32_t number, bool here) : p(p_)
+    {
+        const sl_cache_append_args &a = p.a;
+        const int32_t hd = a.head_dim, half = a.rope_kind ? a.rope_dim / 2 : 0;
+        mine = here && number < p.columns;
+        is_value = number >= p.qk_columns;
+        const int32_t width = is_value ? hd / 4 : hd / U, of_kind = is_value ? number - p.qk_columns : number;
+        // (of_kind / width: under 2^23, and half a column from every whole number of heads)
+        head = (int32_t)(((float)of_kind + 0.5f) * (is_value ? p.inv_value : p.inv_qk));
+        const int32_t k = of_kind - head * width;
+        w0 = VEC ? 4 * k : k;
+        turned = !is_value && w0 < half;
+        split = turned && a.rope_kind == SL_ROPE_HALF;
+        c0 = is_value ? 4 * k : split ? w0 : U * k;
+        const int32_t c1 = split ? w0 + half : c0 + U / 2;
+        const int32_t x_head = (is_value ? a.n_heads + a.n_kv_heads + head : head) * hd;
+        x0 = offset(x_head + c0, p.x_cb, F32 ? 4 : 1);
+        x1 = offset(x_head + c1, p.x_cb, F32 ? 4 : 1);
+        q0 = offset(head * hd + c0, p.q_cb, 1);
+        q1 = offset(head * hd + c1, p.q_cb, 1);
+        k0 = (uint32_t)((head - a.n_heads) << p.shift) * hd + c0;
+        k1 = k0 + (c1 - c0);
+        f = is_value ? p.fv : head < a.n_heads ? p.fq : p.fk;
+    }
+    using Raw = std::conditional_t<F32, f32x4, uint32_t>;
+    __device__ __forceinline__ const int8_t *row(int64_t t) const
+    {
+        return static_cast<const int8_t *>(p.a.x) + token(t, p.cols, p.x_cb, F32 ? 4 : 1);
+    }
+    __device__ __forceinline__ static Raw load4(const int8_t *from, uint32_t by) { return *reinterpret_cast<const Raw *>(from + by); }
+    __device__ __forceinline__ static float load1(const int8_t *from, uint32_t by)
+    {
+        return F32 ? *reinterpret_cast<const float *>(from + by) : (float)from[by];
+    }
+    __device__ __forceinline__ static f32x4 value(Raw v)
+    {
         if constexpr (F32)
-            return *reinterpret_cast<const f32x4 *>(xf + t * p.cols + c);
+            return v;
         else
-            return codes_to_float(*reinterpret_cast<const uint32_t *>(xc + at(t, c, p.cols, p.x_cb)));
-    };
-    const auto load1 = [&](int64_t t, int32_t c) {
-        return F32 ? xf[t * p.cols + c] : (float)xc[at(t, c, p.cols, p.x_cb)];
-    };
-    for (int64_t q4 = ((p0 >> 2) + quad) * 4; q4 < len; q4 += (int64_t)p.quads * 4) {
-        const int64_t lo = max(q4, p0), hi = min(q4 + 4, (int64_t)len);
-        const int32_t n = (int32_t)(hi - lo), skip = (int32_t)(lo - q4);
-        const int64_t t0 = tk.first + (lo - p0);
+            return codes_to_float(v);
+    }
+    // a query's or key's codes: token t's, whose slot's keys of head 0 begin at to_key (NULL: nowhere)
+    template <class C>
+    __device__ __forceinline__ void store(int64_t t, int8_t *to_key, C code0, C code1) const
+    {
+        const sl_cache_append_args &a = p.a;
+        if (head < a.n_heads) {
+            if (a.q) {
+                int8_t *to = a.q + token(t, a.n_heads * a.head_dim, p.q_cb, 1);
+                *reinterpret_cast<C *>(to + q0) = code0;
+                *reinterpret_cast<C *>(to + q1) = code1;
+            }
+        } else if (to_key) {
+            *reinterpret_cast<C *>(to_key + k0) = code0;
+            *reinterpret_cast<C *>(to_key + k1) = code1;
+        }
+    }
+    // a token's part of the column of queries or keys; cs, sn: its angles' cosines and sines
+    __device__ __forceinline__ void turn(int64_t t, Raw r0, Raw r1, const float *cs, const float *sn, int8_t *to_key) const
+    {
+        if constexpr (VEC) {
+            f32x4 y0 = value(r0), y1 = value(r1);
+            if (turned) {
+                const f32x4 c = *reinterpret_cast<const f32x4 *>(cs + w0), s = *reinterpret_cast<const f32x4 *>(sn + w0);
+                const f32x4 x = y0, y = y1;
+                if (p.a.rope_kind == SL_ROPE_HALF) {
+                    y0 = x * c - y * s;
+                    y1 = y * c + x * s;
+                } else {
+                    y0 = f32x4{x[0] * c[0] - x[1] * s[0], x[1] * c[0] + x[0] * s[0], x[2] * c[1] - x[3] * s[1],
+                               x[3] * c[1] + x[2] * s[1]};
+                    y1 = f32x4{y[0] * c[2] - y[1] * s[2], y[1] * c[2] + y[0] * s[2], y[2] * c[3] - y[3] * s[3],
+                               y[3] * c[3] + y[2] * s[3]};
+                }
+            }
+            store(t, to_key, codes_of(y0, f), codes_of(y1, f));
+        } else {
+            float x = load1(row(t), x0), y = load1(row(t), x1);
+            if (turned) {
+                const float c = cs[w0], s = sn[w0], x2 = x * c - y * s;
+                y = y * c + x * s;
+                x = x2;
+            }
+            store(t, to_key, (int8_t)code_bits(x, f), (int8_t)code_bits(y, f));
+        }
+    }
+};
+
+// rope_factor times the cosine and sine of pos * inv_freq[w]. The angle is reduced to
+// quarter turns in 64 bits; within an eighth of a turn, |x| <= pi / 4, the Taylor sums
+// to x^9 and x^10 are within 2^-29 and 2^-31.
+__device__ __forceinline__ void angle(const AppendArgs &p, double pos, int32_t w, float &c, float &s)
+{
+    const double quarters = pos * (double)p.a.inv_freq[w] * 0.63661977236758134308, whole = rint(quarters);
+    const float x = (float)(quarters - whole) * 1.57079632679489662f, x2 = x * x;
+    const uint32_t turn = (uint32_t)(int64_t)whole;
+    float sine = fmaf(x2, 1.0f / 362880.0f, -1.0f / 5040.0f);
+    sine = fmaf(x2, sine, 1.0f / 120.0f);
+    sine = fmaf(x2, sine, -1.0f / 6.0f);
+    sine = fmaf(x * x2, sine, x);
+    float cosine = fmaf(x2, -1.0f / 3628800.0f, 1.0f / 40320.0f);
+    cosine = fmaf(x2, cosine, -1.0f / 720.0f);
+    cosine = fmaf(x2, cosine, 1.0f / 24.0f);
+    cosine = fmaf(x2, cosine, -0.5f);
+    cosine = fmaf(x2, cosine, 1.0f);
+    c = p.a.rope_factor * (turn & 1 ? sine : cosine) * ((turn + 1) & 2 ? -1.0f : 1.0f);
+    s = p.a.rope_factor * (turn & 1 ? cosine : sine) * (turn & 2 ? -1.0f : 1.0f);
+}
+
+// The lengths of a sequence: its tokens of the call and its cached ones.
+__device__ __forceinline__ Tokens lengths(const AppendArgs &p, int32_t seq, int32_t &len)
+{
+    int32_t b0 = ((ScalarTable)(uintptr_t)p.a.seq_start)[seq], b1 = ((ScalarTable)(uintptr_t)p.a.seq_start)[seq + 1];
+    len = ((ScalarTable)(uintptr_t)p.a.kv_len)[seq];
+    asm volatile("" : "+s"(b0), "+s"(b1), "+s"(len));  // (here they are all waited for, instead of one after the other)
+    len = max(len, 0);
+    return tokens_between(b0, b1, p.a.m_tokens);
+}
+
+// The page that holds a slot, or NULL.
+__device__ __forceinline__ int8_t *page_of(const AppendArgs &p, int32_t seq, int64_t slot)
+{
+    const sl_cache_append_args &a = p.a;
+    const int64_t entry = slot >> p.shift;
+    if (slot < 0 || entry >= a.max_pages) return nullptr;
+    const int32_t number = a.page_table[(int64_t)seq * a.max_pages + entry];
+    if ((uint32_t)number >= (uint32_t)a.n_pages) return nullptr;
+    return a.cache + (int64_t)number * (2 * a.n_kv_heads) * ((int64_t)a.head_dim << p.shift);
+}
+
+// One token a sequence: a thread a column, its loads under way while the angles are computed.
+template <bool F32, bool VEC>
+__global__ __launch_bounds__(256) void cache_append_step_kernel(const AppendArgs p)
+{
+    __shared__ __attribute__((aligned(16))) float cs[64], sn[64];
+    const sl_cache_append_args &a = p.a;
+    const int tid = threadIdx.x, seq = p.seq0 + blockIdx.z;
+    int32_t len;
+    const Tokens tk = lengths(p, seq, len);
+    const Column<F32, VEC> col(p, blockIdx.x * p.per + tid, tid < p.per);
+    const int32_t half = a.rope_kind ? a.rope_dim / 2 : 0;
+    for (int32_t i = 0; i < tk.n; ++i) {  // (one, unless a sequence has more than was said)
+        const int64_t t = (int64_t)tk.first + i, slot = (int64_t)len - tk.n + i;
+        typename Column<F32, VEC>::Raw r0{}, r1{};
+        if (col.mine && VEC) {
+            r0 = col.load4(col.row(t), col.x0);
+            if (!col.is_value) r1 = col.load4(col.row(t), col.x1);
+        }
+        int8_t *page = page_of(p, seq, slot);
         if (half) {
             __syncthreads();
-            for (int i = tid; i < n * half; i += 256) {
-                const int32_t j = i / half, w = i % half;
-                const double pos = a.positions ? (double)a.positions[t0 + j] : (double)(lo + j);
-                const double turns = pos * (double)a.inv_freq[w] * 0.15915494309189533577;
-                float s, c;
-                sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
-                cs[j][w] = c * a.rope_factor;
-                sn[j][w] = s * a.rope_factor;
-            }
+            if (tid < half) angle(p, a.positions ? (double)a.positions[t] : (double)slot, tid, cs[tid], sn[tid]);
             __syncthreads();
         }
-        int8_t *page = nullptr;
-        const int64_t entry = q4 >> p.shift;
-        const int32_t in_page = (int32_t)(q4 & ((1 << p.shift) - 1));
-        if (q4 >= 0 && entry < a.max_pages) {
-            const int32_t number = a.page_table[(int64_t)seq * a.max_pages + entry];
-            if ((uint32_t)number < (uint32_t)a.n_pages)
-                page = a.cache + (int64_t)number * (2 * nkv) * ((int64_t)hd << p.shift);
-        }
-        // queries and keys: 8 features (VEC) or 2 a thread
-        constexpr int U = VEC ? 8 : 2;
-        const int32_t units = (nh + nkv) * (hd / U), all = n * units;
-        const auto store = [&](int32_t j, int32_t head, int32_t c, auto code) {
-            using T = decltype(code);
-            if (head < nh) {
-                if (a.q) *reinterpret_cast<T *>(a.q + at(t0 + j, head * hd + c, nh * hd, p.q_cb)) = code;
-            } else if (page) {
-                *reinterpret_cast<T *>(page + (int64_t)(((head - nh) << p.shift) + in_page + skip + j) * hd + c) = code;
-            }
-        };
-        for (int32_t i = part * 256 + tid; i < all; i += p.parts * 256) {
-            const int32_t j = i / units, u = i % units, head = u / (hd / U), k = u % (hd / U);
-            const int64_t t = t0 + j;
-            const float f = head < nh ? p.fq : p.fk;
-            if constexpr (VEC) {
-                const bool turned = 4 * k < half;
-                const bool split = turned && a.rope_kind == SL_ROPE_HALF;
-                const int32_t c0 = split ? 4 * k : 8 * k, c1 = split ? 4 * k + half : 8 * k + 4;
-                f32x4 v0 = load4(t, head * hd + c0), v1 = load4(t, head * hd + c1);
-                if (turned) {
-                    const f32x4 c = *reinterpret_cast<const f32x4 *>(&cs[j][4 * k]);
-                    const f32x4 s = *reinterpret_cast<const f32x4 *>(&sn[j][4 * k]);
-                    const f32x4 x = split ? v0 : f32x4{v0[0], v0[2], v1[0], v1[2]};
-                    const f32x4 y = split ? v1 : f32x4{v0[1], v0[3], v1[1], v1[3]};
-                    const f32x4 x2 = x * c - y * s, y2 = y * c + x * s;
-                    v0 = split ? x2 : f32x4{x2[0], y2[0], x2[1], y2[1]};
-                    v1 = split ? y2 : f32x4{x2[2], y2[2], x2[3], y2[3]};
-                }
-                store(j, head, c0, codes_of(v0, f));
-                store(j, head, c1, codes_of(v1, f));
-            } else {
-                const bool turned = k < half;
-                const bool split = turned && a.rope_kind == SL_ROPE_HALF;
-                const int32_t c0 = split ? k : 2 * k, c1 = split ? k + half : 2 * k + 1;
-                float x = load1(t, head * hd + c0), y = load1(t, head * hd + c1);
-                if (turned) {
-                    const float c = cs[j][k], s = sn[j][k], x2 = x * c - y * s;
-                    y = y * c + x * s;
-                    x = x2;
-                }
-                store(j, head, c0, (int8_t)requant_bits(x, f));
-                store(j, head, c1, (int8_t)requant_bits(y, f));
-            }
-        }
-        if (!page) continue;
-        // values: 4 features of all the slots a thread
-        int8_t *values = page + (int64_t)nkv * ((int64_t)hd << p.shift);
-        for (int32_t i = part * 256 + tid; i < nkv * (hd / 4); i += p.parts * 256) {
-            const int32_t head = i / (hd / 4), c = i % (hd / 4) * 4;
-            int8_t *to = values + ((int64_t)((head << p.shift) + (in_page & ~15)) * hd + c * 16 + (in_page & 15));
-            uint32_t w[4];
+        if (!col.mine) continue;
+        const int32_t in_page = (int32_t)(slot & ((1 << p.shift) - 1));
+        if (!col.is_value) {
+            col.turn(t, r0, r1, cs, sn, page ? page + (int64_t)in_page * a.head_dim : nullptr);
+        } else if (page) {
+            const uint32_t w = codes_of(col.value(VEC ? r0 : col.load4(col.row(t), col.x0)), col.f);
+            int8_t *to = page + (((int64_t)(a.n_kv_heads + col.head) << p.shift) + (in_page & ~15)) * a.head_dim + col.c0 * 16 +
+                         (in_page & 15);
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                w[j] = j < n ? codes_of(load4(t0 + j, (nh + nkv + head) * hd + c), p.fv) : 0;
-            if (n == 4) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    *reinterpret_cast<uint32_t *>(to + 16 * e) =
-                        pack_bytes(w[0] >> (8 * e), w[1] >> (8 * e), w[2] >> (8 * e), w[3] >> (8 * e));
-            } else {
+            for (int e = 0; e < 4; ++e) to[16 * e] = (int8_t)(w >> (8 * e));
+        }
+    }
+}
+
+// Many tokens a sequence. One workgroup: the tokens in 16 consecutive slots, which is
+// what lies together in the values' pages, and `per` columns, kColumns at a time; 4
+// slots of a column a thread, whose loads are all under way before any is used.
+#ifndef APARTS
+#define APARTS 1024.0
+#endif
+constexpr int kColumns = 128;
+template <bool F32, bool VEC>
+__global__ __launch_bounds__(4 * kColumns) __attribute__((amdgpu_waves_per_eu(6))) void cache_append_kernel(const AppendArgs p)
+{
+    __shared__ __attribute__((aligned(16))) float cs[16][64], sn[16][64];
+    __shared__ __attribute__((aligned(16))) uint32_t words[4][kColumns][4];  // 4 tokens' codes of a value's feature
+    const sl_cache_append_args &a = p.a;
+    const int tid = threadIdx.x, seq = p.seq0 + blockIdx.z, here = tid % kColumns;
+    const int quad = __builtin_amdgcn_readfirstlane(tid / kColumns);
+    int32_t len;
+    const Tokens tk = lengths(p, seq, len);
+    if (tk.n == 0) return;
+    const int32_t first_column = blockIdx.x * p.per, end_column = min(first_column + p.per, p.columns);
+    const int32_t half = a.rope_kind && first_column < p.qk_columns ? a.rope_dim / 2 : 0;
+    const int64_t p0 = (int64_t)len - tk.n;  // the first token's slot
+    for (int64_t s0 = (p0 & ~(int64_t)15) + (int64_t)blockIdx.y * 16; s0 < len; s0 += (int64_t)gridDim.y * 16) {
+        const int64_t lo = max(s0, p0), hi = min(s0 + 16, (int64_t)len);
+        // slot j of the thread's is token t0 + j, where there is one
+        const int64_t slot0 = s0 + 4 * quad, t0 = tk.first + (slot0 - p0);
+        const int32_t j0 = (int32_t)min(max(lo - slot0, (int64_t)0), (int64_t)4), j1 = (int32_t)min(max(hi - slot0, (int64_t)0), (int64_t)4);
+        const bool all = hi - lo == 16;
+        int8_t *page = page_of(p, seq, s0);
+        const int32_t in_page = (int32_t)(s0 & ((1 << p.shift) - 1));
+        int8_t *to_key = page ? page + (int64_t)(in_page + 4 * quad) * a.head_dim : nullptr;
+        bool first = true;
+        for (int32_t column = first_column; column < end_column; column += kColumns) {
+            const Column<F32, VEC> col(p, column + here, column + here < end_column);
+            typename Column<F32, VEC>::Raw r0[4]{}, r1[4]{};
+            if (VEC && col.mine) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
+                    if (j >= j0 && j < j1) {
+                        const int8_t *from = col.row(t0 + j);
+                        r0[j] = col.load4(from, col.x0);
+                        if (!col.is_value) r1[j] = col.load4(from, col.x1);
+                    }
+            }
+            if (first && half) {
+                first = false;
+                __syncthreads();
+                const int32_t n = (int32_t)(hi - lo), from = (int32_t)(lo - s0);
+                for (int i = tid; i < n * half; i += 4 * kColumns) {
+                    const int32_t j = i / half, w = i - j * half;
+                    angle(p, a.positions ? (double)a.positions[tk.first + (lo - p0) + j] : (double)(lo + j), w, cs[from + j][w],
+                          sn[from + j][w]);
+                }
+                __syncthreads();
+            }
+            if (!col.is_value && col.mine) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (j < n) to[16 * e + skip + j] = (int8_t)(w[j] >> (8 * e));
+                for (int j = 0; j < 4; ++j)
+                    if (j >= j0 && j < j1)
+                        col.turn(t0 + j, r0[j], r1[j], cs[4 * quad + j], sn[4 * quad + j],
+                                 to_key ? to_key + (int64_t)j * a.head_dim : nullptr);
+            }
+            if (column + kColumns <= p.qk_columns || !page) continue;
+            int8_t *to = page + (((int64_t)(a.n_kv_heads + col.head) << p.shift) + in_page) * a.head_dim + col.c0 * 16;
+            if (col.is_value && col.mine) {
+                uint32_t w[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    w[j] = 0;
+                    if (j >= j0 && j < j1) w[j] = codes_of(col.value(VEC ? r0[j] : col.load4(col.row(t0 + j), col.x0)), col.f);
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t out = pack_bytes(w[0] >> (8 * e), w[1] >> (8 * e), w[2] >> (8 * e), w[3] >> (8 * e));
+                    if (all) {
+                        words[e][here][quad] = out;
+                    } else if (j0 == 0 && j1 == 4) {
+                        *reinterpret_cast<uint32_t *>(to + 16 * e + 4 * quad) = out;
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            if (j >= j0 && j < j1) to[16 * e + 4 * quad + j] = (int8_t)(out >> (8 * j));
+                    }
+                }
+            }
+            if (all) {
+                __syncthreads();
+                if (col.is_value && col.mine)
+                    *reinterpret_cast<i32x4 *>(to + 16 * quad) = *reinterpret_cast<const i32x4 *>(words[quad][here]);
+                __syncthreads();
             }
         }
     }
@@ -540,27 +707,47 @@ sl_status launch_cache_append(const sl_cache_append_args &args, void *stream)
     p.fq = factor(args.q_scale);
     p.fk = factor(args.k_scale);
     p.fv = factor(args.v_scale);
-    p.quads = (args.max_new + 6) / 4;
-    const int64_t groups = (int64_t)p.quads * args.n_seq;
     const bool vec = args.rope_kind == SL_ROPE_NONE || args.rope_dim % 8 == 0;
-    // (a part of the features has a unit a thread at least)
-    p.parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>(512 / groups, p.cols / 8 / 256));
-    const int64_t items = groups * p.parts;
-    if (items > 0x7fffffff / 256) {
+    p.qk_columns = (args.n_heads + args.n_kv_heads) * (args.head_dim / (vec ? 8 : 2));
+    p.columns = p.qk_columns + args.n_kv_heads * (args.head_dim / 4);
+    p.inv_qk = (vec ? 8.0f : 2.0f) / args.head_dim;
+    p.inv_value = 4.0f / args.head_dim;
+    const bool step = args.max_new == 1;
+    constexpr int32_t kMostGrid = 65535;  // workgroups of a launch in its second and third dimension
+    // (the first may begin anywhere in 16 slots; a launch of fewer goes through them in turns)
+    const int64_t groups = step ? 1 : std::min<int64_t>(((int64_t)args.max_new + 30) / 16, kMostGrid);
+    // Features over several workgroups: in a step a column a thread, else until there are enough to fill the CUs.
+    const double tokens = std::min((double)groups * args.n_seq, (double)args.m_tokens / 16 + args.n_seq);
+    int32_t parts = (p.columns + 255) / 256;
+    if (!step) parts = (int32_t)std::max(1.0, std::min((p.columns + kColumns - 1) / kColumns + 0.0, APARTS / tokens));
+    p.per = (p.columns + parts - 1) / parts;
+    if (!step) p.per = (p.per + kColumns - 1) / kColumns * kColumns;
+    parts = (p.columns + p.per - 1) / p.per;
+    if ((double)groups * args.n_seq * parts > 0x7fffffff / (4 * kColumns)) {
         set_error("too many work items for one launch");
         return SL_ERR_UNSUPPORTED;
     }
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    const dim3 grid((uint32_t)items), block(256);
-    if (f32 && vec)
-        hipLaunchKernelGGL((cache_append_kernel<true, true>), grid, block, 0, s, p);
-    else if (f32)
-        hipLaunchKernelGGL((cache_append_kernel<true, false>), grid, block, 0, s, p);
-    else if (vec)
-        hipLaunchKernelGGL((cache_append_kernel<false, true>), grid, block, 0, s, p);
-    else
-        hipLaunchKernelGGL((cache_append_kernel<false, false>), grid, block, 0, s, p);
-    HIP_TRY(hipGetLastError());
+    for (int64_t s0 = 0; s0 < args.n_seq; s0 += kMostGrid) {
+        p.seq0 = (int32_t)s0;
+        const dim3 grid((uint32_t)parts, (uint32_t)groups, (uint32_t)std::min(args.n_seq - p.seq0, kMostGrid));
+        const auto run = [&](auto types, auto width) {
+            constexpr bool F = decltype(types)::value, V = decltype(width)::value;
+            if (step)
+                hipLaunchKernelGGL((cache_append_step_kernel<F, V>), grid, dim3(256), 0, s, p);
+            else
+                hipLaunchKernelGGL((cache_append_kernel<F, V>), grid, dim3(4 * kColumns), 0, s, p);
+        };
+        if (f32 && vec)
+            run(std::true_type{}, std::true_type{});
+        else if (f32)
+            run(std::true_type{}, std::false_type{});
+        else if (vec)
+            run(std::false_type{}, std::true_type{});
+        else
+            run(std::false_type{}, std::false_type{});
+        HIP_TRY(hipGetLastError());
+    }
     return SL_OK;
 }
 

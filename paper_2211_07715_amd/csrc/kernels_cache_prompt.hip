@@ -297,7 +297,9 @@ void cache_prompt_kernel(const CacheArgs a)
         while (c < mine) {
             bring();
             scores(lds + buf, from_z(), sc);
-            mask(c, gone, sc);
+            // (where the two sides take turns the first chunk is a large part of all, and mostly seen whole; elsewhere the
+            // branch costs more than it saves: 32 x 512 tokens of 12 heads 36.8 us against 34.7)
+            if (RW == 4 || kChunk * (c + 1) > least || gone) mask(c, gone, sc);
             const int32_t by = raise(largest(sc));
             // (what is masked stays far below everything, as a finite number)
 #pragma unroll
@@ -325,40 +327,38 @@ void cache_prompt_kernel(const CacheArgs a)
         // a lane half holds features 16 N half .. 16 N half + 16 N - 1 of its query
         float sum = pair_sum(l);
         if constexpr (KW > 1) {
-            // what the parts after the first have goes to it, all from the largest m
-            __shared__ int32_t zs[KW][TQ];
-            __shared__ float ls[KW][TQ];
+            // what the other parts have goes to the first, which puts all on the largest m
+            __shared__ int32_t zs[KW - 1][TQ];
+            __shared__ float ls[KW - 1][TQ];
             const int row = wave * 32 + n32;
-            if (half == 0) zs[part][row] = z;
-            __syncthreads();
-            int32_t least_z = zs[0][row];
-#pragma unroll
-            for (int k = 1; k < KW; ++k) least_z = min(least_z, zs[k][row]);
-            const float f = __builtin_amdgcn_exp2f(-(float)(z - least_z) * a.c2);
-            z = least_z;
-            sum *= f;
-            float *mine_o = reinterpret_cast<float *>(all_lds) + ((part - 1) * RW + wave) * (1024 * N) + lane;
-#pragma unroll
-            for (int d = 0; d < N; ++d)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    o[d][e] *= f;
-                    if (part) mine_o[64 * (16 * d + e)] = o[d][e];
+            float *to = reinterpret_cast<float *>(all_lds) + lane;
+            if (part) {
+                if (half == 0) {
+                    zs[part - 1][row] = z;
+                    ls[part - 1][row] = sum;
                 }
-            if (half == 0) ls[part][row] = sum;
+#pragma unroll
+                for (int d = 0; d < N; ++d)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) to[((part - 1) * RW + wave) * (1024 * N) + 64 * (16 * d + e)] = o[d][e];
+            }
             __syncthreads();
             if (part == 0) {
 #pragma unroll
-                for (int k = 1; k < KW; ++k) {
-                    sum += ls[k][row];
-                    const float *from = reinterpret_cast<const float *>(all_lds) + ((k - 1) * RW + wave) * (1024 * N) + lane;
+                for (int k = 0; k < KW - 1; ++k) {
+                    const int32_t z2 = zs[k][row], least_z = min(z, z2);
+                    const float f = __builtin_amdgcn_exp2f(-(float)(z - least_z) * a.c2);
+                    const float f2 = __builtin_amdgcn_exp2f(-(float)(z2 - least_z) * a.c2);
+                    z = least_z;
+                    sum = sum * f + ls[k][row] * f2;
 #pragma unroll
                     for (int d = 0; d < N; ++d)
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) o[d][e] += from[64 * (16 * d + e)];
+                        for (int e = 0; e < 16; ++e)
+                            o[d][e] = o[d][e] * f + to[(k * RW + wave) * (1024 * N) + 64 * (16 * d + e)] * f2;
                 }
             }
-            __syncthreads();  // (before the next tile's keys come)
+            if ((tile + a.tiles) * TQ < rows) __syncthreads();  // (before the next tile's keys come)
             if (part) continue;
         }
         const int32_t i = query(head);
