@@ -15,12 +15,18 @@ namespace {
 // --- cache_append --------------------------------------------------------------
 
 struct AppendArgs {
-    sl_cache_append_args a;
-    int32_t cols, x_cb, q_cb, shift;  // 1 << shift: tokens of a page
-    int32_t qk_columns, columns, per;  // a thread each: of queries and keys, and of all; `per` a workgroup
-    int32_t seq0;
-    float fq, fk, fv;  // from x's unit to the codes'
-    float inv_qk, inv_value;  // 1 / columns of a head
+    const int8_t *x;
+    int8_t *q, *cache;
+    const int32_t *seq_start, *kv_len, *page_table, *positions;
+    const float *inv_freq;
+    int64_t m;
+    int32_t seq0, max_pages, n_pages, shift;  // 1 << shift: tokens of a page
+    int32_t nh, nkv, hd, cols, x_cb, q_cb;
+    int32_t half, split;                      // rotated pairs of a head; 1: (j, j + half), 0: (2 j, 2 j + 1)
+    int32_t q_columns, k_columns, v_columns;  // a thread each
+    int32_t q_parts, k_parts, per, v_per;     // workgroups of queries and of keys, and columns of one
+    float rope_factor, fq, fk, fv;            // f*: from x's unit to the codes'
+    float inv_qk, inv_value, inv_half;        // 1 / columns of a head, and of its rotated pairs
 };
 
 __device__ __forceinline__ f32x4 codes_to_float(uint32_t w)
@@ -39,93 +45,70 @@ __device__ __forceinline__ uint32_t codes_of(f32x4 v, float f)
     return pack_bytes(code_bits(v[0], f), code_bits(v[1], f), code_bits(v[2], f), code_bits(v[3], f));
 }
 
+// 4 x 4 bytes: byte j of word e becomes byte e of word j.
+__device__ __forceinline__ void transpose_bytes(uint32_t (&w)[4])
+{
+    const uint32_t a = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), b = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u);
+    const uint32_t c = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u), d = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
+    w[0] = __builtin_amdgcn_perm(c, a, 0x05040100u);
+    w[1] = __builtin_amdgcn_perm(c, a, 0x07060302u);
+    w[2] = __builtin_amdgcn_perm(d, b, 0x05040100u);
+    w[3] = __builtin_amdgcn_perm(d, b, 0x07060302u);
+}
+
+// A token's place in an activation, the same for a wave, and a feature's from there.
+__device__ __forceinline__ int64_t row_offset(int64_t t, int32_t cols, int32_t cb, int32_t size)
+{
+    return cb ? (t >> 4) * cb * 512 + (t & 15) * 32 : t * cols * size;
+}
+__device__ __forceinline__ uint32_t feature_offset(int32_t c, int32_t cb, int32_t size)
+{
+    return cb ? (uint32_t)(c >> 5) * 512 + (c & 31) : (uint32_t)c * size;
+}
+
 // What a thread does: a column, which is 8 features of a query or key head (VEC:
 // rope_dim is a multiple of 8, so that 4 features of both halves of pairs lie
-// together; else 2 features), or 4 features of a value head.
+// together; else 2 features), or 4 features of a value head. A workgroup's columns
+// are all of queries, of keys or of values.
 template <bool F32, bool VEC>
-struct Column {
+struct PairColumn {
     static constexpr int U = VEC ? 8 : 2;
-    const AppendArgs &p;
-    bool mine, is_value, turned, split;
-    int32_t head, w0, c0;     // first angle, first feature
-    uint32_t x0, x1, q0, q1;  // bytes of both parts from a token's first in x and q,
-    uint32_t k0, k1;          // and from a slot's of head 0 in a page's keys
-    float f;
-    // A token's place is the same for all lanes, a column's the same for all tokens: addresses are sums of the two.
-    __device__ __forceinline__ static uint32_t offset(int32_t c, int32_t cb, int32_t size)
+    using Raw = std::conditional_t<VEC, std::conditional_t<F32, f32x4, uint32_t>, std::conditional_t<F32, float, int8_t>>;
+    int32_t w0;               // first angle
+    bool turned;
+    uint32_t x0, x1, d0, d1;  // bytes of both parts from a token's first: in x, and where their codes go
+    __device__ __forceinline__ PairColumn(const AppendArgs &p, int32_t number, bool keys)
     {
-        return cb ? (uint32_t)(c >> 5) * 512 + (c & 31) : (uint32_t)c * size;
-    }
-    __device__ __forceinline__ static int64_t token(int64_t t, int32_t cols, int32_t cb, int32_t size)
-    {
-        return cb ? (t >> 4) * cb * 512 + (t & 15) * 32 : t * cols * size;
-    }
-    __device__ __forceinline__ Column(const AppendArgs &p_, int32_t number, bool here) : p(p_)
-    {
-        const sl_cache_append_args &a = p.a;
-        const int32_t hd = a.head_dim, half = a.rope_kind ? a.rope_dim / 2 : 0;
-        mine = here && number < p.columns;
-        is_value = number >= p.qk_columns;
-        const int32_t width = is_value ? hd / 4 : hd / U, of_kind = is_value ? number - p.qk_columns : number;
-        // (of_kind / width: under 2^23, and half a column from every whole number of heads)
-        head = (int32_t)(((float)of_kind + 0.5f) * (is_value ? p.inv_value : p.inv_qk));
-        const int32_t k = of_kind - head * width;
+        // (number / columns of a head: under 2^23, and half a column from every whole number of heads)
+        const int32_t head = (int32_t)(((float)number + 0.5f) * p.inv_qk), k = number - head * (p.hd / U);
         w0 = VEC ? 4 * k : k;
-        turned = !is_value && w0 < half;
-        split = turned && a.rope_kind == SL_ROPE_HALF;
-        c0 = is_value ? 4 * k : split ? w0 : U * k;
-        const int32_t c1 = split ? w0 + half : c0 + U / 2;
-        const int32_t x_head = (is_value ? a.n_heads + a.n_kv_heads + head : head) * hd;
-        x0 = offset(x_head + c0, p.x_cb, F32 ? 4 : 1);
-        x1 = offset(x_head + c1, p.x_cb, F32 ? 4 : 1);
-        q0 = offset(head * hd + c0, p.q_cb, 1);
-        q1 = offset(head * hd + c1, p.q_cb, 1);
-        k0 = (uint32_t)((head - a.n_heads) << p.shift) * hd + c0;
-        k1 = k0 + (c1 - c0);
-        f = is_value ? p.fv : head < a.n_heads ? p.fq : p.fk;
+        turned = w0 < p.half;
+        const bool apart = turned && p.split;
+        const int32_t c0 = apart ? w0 : U * k, c1 = apart ? w0 + p.half : c0 + U / 2;
+        const int32_t x_head = (keys ? p.nh + head : head) * p.hd;
+        x0 = feature_offset(x_head + c0, p.x_cb, F32 ? 4 : 1);
+        x1 = feature_offset(x_head + c1, p.x_cb, F32 ? 4 : 1);
+        d0 = keys ? (uint32_t)(head << p.shift) * p.hd + c0 : feature_offset(head * p.hd + c0, p.q_cb, 1);
+        d1 = keys ? d0 + (c1 - c0) : feature_offset(head * p.hd + c1, p.q_cb, 1);
     }
-    using Raw = std::conditional_t<F32, f32x4, uint32_t>;
-    __device__ __forceinline__ const int8_t *row(int64_t t) const
-    {
-        return static_cast<const int8_t *>(p.a.x) + token(t, p.cols, p.x_cb, F32 ? 4 : 1);
-    }
-    __device__ __forceinline__ static Raw load4(const int8_t *from, uint32_t by) { return *reinterpret_cast<const Raw *>(from + by); }
-    __device__ __forceinline__ static float load1(const int8_t *from, uint32_t by)
-    {
-        return F32 ? *reinterpret_cast<const float *>(from + by) : (float)from[by];
-    }
-    __device__ __forceinline__ static f32x4 value(Raw v)
-    {
-        if constexpr (F32)
-            return v;
-        else
-            return codes_to_float(v);
-    }
-    // a query's or key's codes: token t's, whose slot's keys of head 0 begin at to_key (NULL: nowhere)
-    template <class C>
-    __device__ __forceinline__ void store(int64_t t, int8_t *to_key, C code0, C code1) const
-    {
-        const sl_cache_append_args &a = p.a;
-        if (head < a.n_heads) {
-            if (a.q) {
-                int8_t *to = a.q + token(t, a.n_heads * a.head_dim, p.q_cb, 1);
-                *reinterpret_cast<C *>(to + q0) = code0;
-                *reinterpret_cast<C *>(to + q1) = code1;
-            }
-        } else if (to_key) {
-            *reinterpret_cast<C *>(to_key + k0) = code0;
-            *reinterpret_cast<C *>(to_key + k1) = code1;
-        }
-    }
-    // a token's part of the column of queries or keys; cs, sn: its angles' cosines and sines
-    __device__ __forceinline__ void turn(int64_t t, Raw r0, Raw r1, const float *cs, const float *sn, int8_t *to_key) const
+    __device__ __forceinline__ static Raw load(const int8_t *row, uint32_t by) { return *reinterpret_cast<const Raw *>(row + by); }
+    // a token's codes: cs, sn are its angles' cosines and sines, its row of codes begins at `to`
+    __device__ __forceinline__ void put(const AppendArgs &p, Raw r0, Raw r1, const float *cs, const float *sn, int8_t *to,
+                                        float f) const
     {
         if constexpr (VEC) {
-            f32x4 y0 = value(r0), y1 = value(r1);
+            f32x4 y0, y1;
+            if constexpr (F32) {
+                y0 = r0;
+                y1 = r1;
+            } else {
+                y0 = codes_to_float(r0);
+                y1 = codes_to_float(r1);
+            }
             if (turned) {
                 const f32x4 c = *reinterpret_cast<const f32x4 *>(cs + w0), s = *reinterpret_cast<const f32x4 *>(sn + w0);
                 const f32x4 x = y0, y = y1;
-                if (p.a.rope_kind == SL_ROPE_HALF) {
+                if (p.split) {
                     y0 = x * c - y * s;
                     y1 = y * c + x * s;
                 } else {
@@ -135,16 +118,38 @@ struct Column {
                                y[3] * c[3] + y[2] * s[3]};
                 }
             }
-            store(t, to_key, codes_of(y0, f), codes_of(y1, f));
+            *reinterpret_cast<uint32_t *>(to + d0) = codes_of(y0, f);
+            *reinterpret_cast<uint32_t *>(to + d1) = codes_of(y1, f);
         } else {
-            float x = load1(row(t), x0), y = load1(row(t), x1);
+            float x = (float)r0, y = (float)r1;
             if (turned) {
                 const float c = cs[w0], s = sn[w0], x2 = x * c - y * s;
                 y = y * c + x * s;
                 x = x2;
             }
-            store(t, to_key, (int8_t)code_bits(x, f), (int8_t)code_bits(y, f));
+            to[d0] = (int8_t)code_bits(x, f);
+            to[d1] = (int8_t)code_bits(y, f);
         }
+    }
+};
+
+template <bool F32>
+struct ValueColumn {
+    using Raw = std::conditional_t<F32, f32x4, uint32_t>;
+    uint32_t x0, d0;  // bytes from a token's first in x, and from a page's first value in a group of 16 tokens
+    __device__ __forceinline__ ValueColumn(const AppendArgs &p, int32_t number)
+    {
+        const int32_t head = (int32_t)(((float)number + 0.5f) * p.inv_value), c = 4 * (number - head * (p.hd / 4));
+        x0 = feature_offset((p.nh + p.nkv + head) * p.hd + c, p.x_cb, F32 ? 4 : 1);
+        d0 = (uint32_t)(head << p.shift) * p.hd + c * 16;
+    }
+    __device__ __forceinline__ Raw load(const int8_t *row) const { return *reinterpret_cast<const Raw *>(row + x0); }
+    __device__ __forceinline__ static uint32_t codes(const AppendArgs &p, Raw r)
+    {
+        if constexpr (F32)
+            return codes_of(r, p.fv);
+        else
+            return codes_of(codes_to_float(r), p.fv);
     }
 };
 
@@ -153,7 +158,7 @@ struct Column {
 // to x^9 and x^10 are within 2^-29 and 2^-31.
 __device__ __forceinline__ void angle(const AppendArgs &p, double pos, int32_t w, float &c, float &s)
 {
-    const double quarters = pos * (double)p.a.inv_freq[w] * 0.63661977236758134308, whole = rint(quarters);
+    const double quarters = pos * (double)p.inv_freq[w] * 0.63661977236758134308, whole = rint(quarters);
     const float x = (float)(quarters - whole) * 1.57079632679489662f, x2 = x * x;
     const uint32_t turn = (uint32_t)(int64_t)whole;
     float sine = fmaf(x2, 1.0f / 362880.0f, -1.0f / 5040.0f);
@@ -165,29 +170,41 @@ __device__ __forceinline__ void angle(const AppendArgs &p, double pos, int32_t w
     cosine = fmaf(x2, cosine, 1.0f / 24.0f);
     cosine = fmaf(x2, cosine, -0.5f);
     cosine = fmaf(x2, cosine, 1.0f);
-    c = p.a.rope_factor * (turn & 1 ? sine : cosine) * ((turn + 1) & 2 ? -1.0f : 1.0f);
-    s = p.a.rope_factor * (turn & 1 ? cosine : sine) * (turn & 2 ? -1.0f : 1.0f);
+    c = p.rope_factor * (turn & 1 ? sine : cosine) * ((turn + 1) & 2 ? -1.0f : 1.0f);
+    s = p.rope_factor * (turn & 1 ? cosine : sine) * (turn & 2 ? -1.0f : 1.0f);
 }
 
 // The lengths of a sequence: its tokens of the call and its cached ones.
 __device__ __forceinline__ Tokens lengths(const AppendArgs &p, int32_t seq, int32_t &len)
 {
-    int32_t b0 = ((ScalarTable)(uintptr_t)p.a.seq_start)[seq], b1 = ((ScalarTable)(uintptr_t)p.a.seq_start)[seq + 1];
-    len = ((ScalarTable)(uintptr_t)p.a.kv_len)[seq];
+    int32_t b0 = ((ScalarTable)(uintptr_t)p.seq_start)[seq], b1 = ((ScalarTable)(uintptr_t)p.seq_start)[seq + 1];
+    len = ((ScalarTable)(uintptr_t)p.kv_len)[seq];
     asm volatile("" : "+s"(b0), "+s"(b1), "+s"(len));  // (here they are all waited for, instead of one after the other)
     len = max(len, 0);
-    return tokens_between(b0, b1, p.a.m_tokens);
+    return tokens_between(b0, b1, p.m);
 }
 
 // The page that holds a slot, or NULL.
 __device__ __forceinline__ int8_t *page_of(const AppendArgs &p, int32_t seq, int64_t slot)
 {
-    const sl_cache_append_args &a = p.a;
     const int64_t entry = slot >> p.shift;
-    if (slot < 0 || entry >= a.max_pages) return nullptr;
-    const int32_t number = a.page_table[(int64_t)seq * a.max_pages + entry];
-    if ((uint32_t)number >= (uint32_t)a.n_pages) return nullptr;
-    return a.cache + (int64_t)number * (2 * a.n_kv_heads) * ((int64_t)a.head_dim << p.shift);
+    if (slot < 0 || entry >= p.max_pages) return nullptr;
+    const int32_t number = ((ScalarTable)(uintptr_t)p.page_table)[(int64_t)seq * p.max_pages + entry];
+    if ((uint32_t)number >= (uint32_t)p.n_pages) return nullptr;
+    return p.cache + (int64_t)number * (2 * p.nkv) * ((int64_t)p.hd << p.shift);
+}
+
+// Which columns a workgroup has: `first` to `end` of the queries (0), keys (1) or values (2).
+struct Share {
+    int32_t kind, first, end;
+};
+__device__ __forceinline__ Share share_of(const AppendArgs &p, int32_t part)
+{
+    if (part < p.q_parts) return {0, part * p.per, min((part + 1) * p.per, p.q_columns)};
+    part -= p.q_parts;
+    if (part < p.k_parts) return {1, part * p.per, min((part + 1) * p.per, p.k_columns)};
+    part -= p.k_parts;
+    return {2, part * p.v_per, min((part + 1) * p.v_per, p.v_columns)};
 }
 
 // One token a sequence: a thread a column, its loads under way while the angles are computed.
@@ -195,128 +212,150 @@ template <bool F32, bool VEC>
 __global__ __launch_bounds__(256) void cache_append_step_kernel(const AppendArgs p)
 {
     __shared__ __attribute__((aligned(16))) float cs[64], sn[64];
-    const sl_cache_append_args &a = p.a;
     const int tid = threadIdx.x, seq = p.seq0 + blockIdx.z;
+    const Share my = share_of(p, blockIdx.x);
+    const int32_t column = my.first + tid;
+    const bool mine = column < my.end;
     int32_t len;
     const Tokens tk = lengths(p, seq, len);
-    const Column<F32, VEC> col(p, blockIdx.x * p.per + tid, tid < p.per);
-    const int32_t half = a.rope_kind ? a.rope_dim / 2 : 0;
     for (int32_t i = 0; i < tk.n; ++i) {  // (one, unless a sequence has more than was said)
         const int64_t t = (int64_t)tk.first + i, slot = (int64_t)len - tk.n + i;
-        typename Column<F32, VEC>::Raw r0{}, r1{};
-        if (col.mine && VEC) {
-            r0 = col.load4(col.row(t), col.x0);
-            if (!col.is_value) r1 = col.load4(col.row(t), col.x1);
-        }
-        int8_t *page = page_of(p, seq, slot);
-        if (half) {
-            __syncthreads();
-            if (tid < half) angle(p, a.positions ? (double)a.positions[t] : (double)slot, tid, cs[tid], sn[tid]);
-            __syncthreads();
-        }
-        if (!col.mine) continue;
+        const int8_t *row = p.x + row_offset(t, p.cols, p.x_cb, F32 ? 4 : 1);
         const int32_t in_page = (int32_t)(slot & ((1 << p.shift) - 1));
-        if (!col.is_value) {
-            col.turn(t, r0, r1, cs, sn, page ? page + (int64_t)in_page * a.head_dim : nullptr);
-        } else if (page) {
-            const uint32_t w = codes_of(col.value(VEC ? r0 : col.load4(col.row(t), col.x0)), col.f);
-            int8_t *to = page + (((int64_t)(a.n_kv_heads + col.head) << p.shift) + (in_page & ~15)) * a.head_dim + col.c0 * 16 +
-                         (in_page & 15);
+        if (my.kind == 2) {
+            const ValueColumn<F32> col(p, column);
+            typename ValueColumn<F32>::Raw r{};
+            if (mine) r = col.load(row);
+            int8_t *page = page_of(p, seq, slot);
+            if (!page || !mine) continue;
+            int8_t *to = page + ((int64_t)p.nkv << p.shift) * p.hd + (in_page & ~15) * p.hd + (in_page & 15);
+            const uint32_t w = col.codes(p, r);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) to[16 * e] = (int8_t)(w >> (8 * e));
+            for (int e = 0; e < 4; ++e) (to + 16 * e)[col.d0] = (int8_t)(w >> (8 * e));
+        } else {
+            const PairColumn<F32, VEC> col(p, column, my.kind == 1);
+            typename PairColumn<F32, VEC>::Raw r0{}, r1{};
+            if (mine) {
+                r0 = col.load(row, col.x0);
+                r1 = col.load(row, col.x1);
+            }
+            int8_t *page = my.kind ? page_of(p, seq, slot) : nullptr;
+            if (p.half) {
+                __syncthreads();
+                if (tid < p.half) angle(p, p.positions ? (double)p.positions[t] : (double)slot, tid, cs[tid], sn[tid]);
+                __syncthreads();
+            }
+            if (!mine || (my.kind && !page)) continue;
+            col.put(p, r0, r1, cs, sn, my.kind ? page + (int64_t)in_page * p.hd : p.q + row_offset(t, p.nh * p.hd, p.q_cb, 1),
+                    my.kind ? p.fk : p.fq);
         }
     }
 }
 
 // Many tokens a sequence. One workgroup: the tokens in 16 consecutive slots, which is
-// what lies together in the values' pages, and `per` columns, kColumns at a time; 4
-// slots of a column a thread, whose loads are all under way before any is used.
-#ifndef APARTS
-#define APARTS 1024.0
-#endif
-constexpr int kColumns = 128;
+// what lies together in the values' pages, and some columns, 64 at a time; a wave has
+// 4 of the slots, whose loads are all under way before any is used.
 template <bool F32, bool VEC>
-__global__ __launch_bounds__(4 * kColumns) __attribute__((amdgpu_waves_per_eu(6))) void cache_append_kernel(const AppendArgs p)
+__global__ __launch_bounds__(256) void cache_append_kernel(const AppendArgs p)
 {
     __shared__ __attribute__((aligned(16))) float cs[16][64], sn[16][64];
-    __shared__ __attribute__((aligned(16))) uint32_t words[4][kColumns][4];  // 4 tokens' codes of a value's feature
-    const sl_cache_append_args &a = p.a;
-    const int tid = threadIdx.x, seq = p.seq0 + blockIdx.z, here = tid % kColumns;
-    const int quad = __builtin_amdgcn_readfirstlane(tid / kColumns);
+    __shared__ __attribute__((aligned(16))) uint32_t words[4][64][4];  // 4 tokens' codes of a value's feature
+    const int tid = threadIdx.x, lane = tid & 63, quad = __builtin_amdgcn_readfirstlane(tid >> 6), seq = p.seq0 + blockIdx.z;
+    const Share my = share_of(p, blockIdx.x);
     int32_t len;
     const Tokens tk = lengths(p, seq, len);
-    if (tk.n == 0) return;
-    const int32_t first_column = blockIdx.x * p.per, end_column = min(first_column + p.per, p.columns);
-    const int32_t half = a.rope_kind && first_column < p.qk_columns ? a.rope_dim / 2 : 0;
     const int64_t p0 = (int64_t)len - tk.n;  // the first token's slot
-    for (int64_t s0 = (p0 & ~(int64_t)15) + (int64_t)blockIdx.y * 16; s0 < len; s0 += (int64_t)gridDim.y * 16) {
-        const int64_t lo = max(s0, p0), hi = min(s0 + 16, (int64_t)len);
-        // slot j of the thread's is token t0 + j, where there is one
-        const int64_t slot0 = s0 + 4 * quad, t0 = tk.first + (slot0 - p0);
-        const int32_t j0 = (int32_t)min(max(lo - slot0, (int64_t)0), (int64_t)4), j1 = (int32_t)min(max(hi - slot0, (int64_t)0), (int64_t)4);
-        const bool all = hi - lo == 16;
-        int8_t *page = page_of(p, seq, s0);
+    for (int64_t s0 = (p0 & ~(int64_t)15) + (int64_t)blockIdx.y * 16; s0 < len && tk.n; s0 += (int64_t)gridDim.y * 16) {
+        // slots from .. to - 1 of the 16 have a token, j0 .. j1 - 1 of the wave's 4
+        const int32_t from = (int32_t)(max(s0, p0) - s0), to = (int32_t)(min(s0 + 16, (int64_t)len) - s0);
+        const int32_t j0 = min(max(from - 4 * quad, 0), 4), j1 = min(max(to - 4 * quad, 0), 4);
+        const int64_t t0 = tk.first + (s0 - p0);  // slot j's token is t0 + j
+        const auto row = [&](int32_t j) { return p.x + row_offset(t0 + 4 * quad + j, p.cols, p.x_cb, F32 ? 4 : 1); };
         const int32_t in_page = (int32_t)(s0 & ((1 << p.shift) - 1));
-        int8_t *to_key = page ? page + (int64_t)(in_page + 4 * quad) * a.head_dim : nullptr;
-        bool first = true;
-        for (int32_t column = first_column; column < end_column; column += kColumns) {
-            const Column<F32, VEC> col(p, column + here, column + here < end_column);
-            typename Column<F32, VEC>::Raw r0[4]{}, r1[4]{};
-            if (VEC && col.mine) {
+        int8_t *page = my.kind ? page_of(p, seq, s0) : nullptr;
+        if (my.kind == 2) {
+            if (!page) continue;
+            int8_t *group = page + ((int64_t)p.nkv << p.shift) * p.hd + in_page * p.hd;
+            for (int32_t column = my.first; column < my.end; column += 64) {
+                const bool mine = column + lane < my.end;
+                const ValueColumn<F32> col(p, column + lane);
+                typename ValueColumn<F32>::Raw r[4]{};
+                if (j1 - j0 == 4) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (j >= j0 && j < j1) {
-                        const int8_t *from = col.row(t0 + j);
-                        r0[j] = col.load4(from, col.x0);
-                        if (!col.is_value) r1[j] = col.load4(from, col.x1);
-                    }
-            }
-            if (first && half) {
-                first = false;
-                __syncthreads();
-                const int32_t n = (int32_t)(hi - lo), from = (int32_t)(lo - s0);
-                for (int i = tid; i < n * half; i += 4 * kColumns) {
-                    const int32_t j = i / half, w = i - j * half;
-                    angle(p, a.positions ? (double)a.positions[tk.first + (lo - p0) + j] : (double)(lo + j), w, cs[from + j][w],
-                          sn[from + j][w]);
+                    for (int j = 0; j < 4; ++j)
+                        if (mine) r[j] = col.load(row(j));
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (mine && j >= j0 && j < j1) r[j] = col.load(row(j));
                 }
-                __syncthreads();
-            }
-            if (!col.is_value && col.mine) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (j >= j0 && j < j1)
-                        col.turn(t0 + j, r0[j], r1[j], cs[4 * quad + j], sn[4 * quad + j],
-                                 to_key ? to_key + (int64_t)j * a.head_dim : nullptr);
-            }
-            if (column + kColumns <= p.qk_columns || !page) continue;
-            int8_t *to = page + (((int64_t)(a.n_kv_heads + col.head) << p.shift) + in_page) * a.head_dim + col.c0 * 16;
-            if (col.is_value && col.mine) {
                 uint32_t w[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    w[j] = 0;
-                    if (j >= j0 && j < j1) w[j] = codes_of(col.value(VEC ? r0[j] : col.load4(col.row(t0 + j), col.x0)), col.f);
-                }
+                for (int j = 0; j < 4; ++j) w[j] = col.codes(p, r[j]);
+                // features e = 0 .. 3, a word of 4 tokens each
+                transpose_bytes(w);
+                if (to - from == 16) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t out = pack_bytes(w[0] >> (8 * e), w[1] >> (8 * e), w[2] >> (8 * e), w[3] >> (8 * e));
-                    if (all) {
-                        words[e][here][quad] = out;
-                    } else if (j0 == 0 && j1 == 4) {
-                        *reinterpret_cast<uint32_t *>(to + 16 * e + 4 * quad) = out;
-                    } else {
+                    for (int e = 0; e < 4; ++e) words[e][lane][quad] = w[e];
+                    __syncthreads();
+                    if (mine)
+                        *reinterpret_cast<i32x4 *>(group + 16 * quad + col.d0) =
+                            *reinterpret_cast<const i32x4 *>(words[quad][lane]);
+                    __syncthreads();
+                } else if (mine) {
 #pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            if (j >= j0 && j < j1) to[16 * e + 4 * quad + j] = (int8_t)(out >> (8 * j));
+                    for (int e = 0; e < 4; ++e) {
+                        int8_t *at = group + 16 * e + 4 * quad + col.d0;
+                        if (j1 - j0 == 4)
+                            *reinterpret_cast<uint32_t *>(at) = w[e];
+                        else
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                if (j >= j0 && j < j1) at[j] = (int8_t)(w[e] >> (8 * j));
                     }
                 }
             }
-            if (all) {
-                __syncthreads();
-                if (col.is_value && col.mine)
-                    *reinterpret_cast<i32x4 *>(to + 16 * quad) = *reinterpret_cast<const i32x4 *>(words[quad][here]);
-                __syncthreads();
+            continue;
+        }
+        if (my.kind && !page) continue;
+        if (p.half) {
+            __syncthreads();
+            // (a wave the angles of its own slots; their number divides by no more than 64 rotated pairs)
+            for (int32_t i = lane; i < 4 * p.half; i += 64) {
+                const int32_t j = (int32_t)(((float)i + 0.5f) * p.inv_half), w = i - j * p.half;
+                if (j >= j0 && j < j1)
+                    angle(p, p.positions ? (double)p.positions[t0 + 4 * quad + j] : (double)(s0 + 4 * quad + j), w,
+                          cs[4 * quad + j][w], sn[4 * quad + j][w]);
+            }
+            __syncthreads();
+        }
+        const auto code_row = [&](int32_t j) {
+            return my.kind ? page + (int64_t)(in_page + 4 * quad + j) * p.hd
+                           : p.q + row_offset(t0 + 4 * quad + j, p.nh * p.hd, p.q_cb, 1);
+        };
+        const float f = my.kind ? p.fk : p.fq;
+        for (int32_t column = my.first + lane; column < my.end; column += 64) {
+            const PairColumn<F32, VEC> col(p, column, my.kind == 1);
+            if (j1 - j0 == 4) {
+                typename PairColumn<F32, VEC>::Raw r0[4], r1[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    r0[j] = col.load(row(j), col.x0);
+                    r1[j] = col.load(row(j), col.x1);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) col.put(p, r0[j], r1[j], cs[4 * quad + j], sn[4 * quad + j], code_row(j), f);
+            } else {
+                typename PairColumn<F32, VEC>::Raw r0[4]{}, r1[4]{};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (j < j0 || j >= j1) continue;
+                    r0[j] = col.load(row(j), col.x0);
+                    r1[j] = col.load(row(j), col.x1);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (j >= j0 && j < j1) col.put(p, r0[j], r1[j], cs[4 * quad + j], sn[4 * quad + j], code_row(j), f);
             }
         }
     }
@@ -694,49 +733,75 @@ int64_t cache_attention_bytes(const sl_cache_attention_args &a)
     return (int64_t)a.n_seq * a.n_kv_heads * p.tiles * p.splits * record(a.head_dim, p.tile_rows) * 4;
 }
 
-sl_status launch_cache_append(const sl_cache_append_args &args, void *stream)
+sl_status launch_cache_append(const sl_cache_append_args &a, void *stream)
 {
+    const bool f32 = a.x_type == SL_ACT_F32, vec = a.rope_kind == SL_ROPE_NONE || a.rope_dim % 8 == 0;
     AppendArgs p{};
-    p.a = args;
-    p.cols = (args.n_heads + 2 * args.n_kv_heads) * args.head_dim;
-    const bool f32 = args.x_type == SL_ACT_F32;
-    p.x_cb = !f32 && args.x_layout == SL_LAYOUT_T16X32 ? (p.cols + 31) / 32 : 0;
-    p.q_cb = args.q_layout == SL_LAYOUT_T16X32 ? (args.n_heads * args.head_dim + 31) / 32 : 0;
-    p.shift = __builtin_ctz(args.page_size);
-    const auto factor = [&](float scale) { return f32 ? 1.0f / scale : (float)((double)args.x_scale / scale); };
-    p.fq = factor(args.q_scale);
-    p.fk = factor(args.k_scale);
-    p.fv = factor(args.v_scale);
-    const bool vec = args.rope_kind == SL_ROPE_NONE || args.rope_dim % 8 == 0;
-    p.qk_columns = (args.n_heads + args.n_kv_heads) * (args.head_dim / (vec ? 8 : 2));
-    p.columns = p.qk_columns + args.n_kv_heads * (args.head_dim / 4);
-    p.inv_qk = (vec ? 8.0f : 2.0f) / args.head_dim;
-    p.inv_value = 4.0f / args.head_dim;
-    const bool step = args.max_new == 1;
+    p.x = static_cast<const int8_t *>(a.x);
+    p.q = a.q;
+    p.cache = a.cache;
+    p.seq_start = a.seq_start;
+    p.kv_len = a.kv_len;
+    p.page_table = a.page_table;
+    p.positions = a.positions;
+    p.inv_freq = a.inv_freq;
+    p.m = a.m_tokens;
+    p.max_pages = a.max_pages;
+    p.n_pages = a.n_pages;
+    p.shift = __builtin_ctz(a.page_size);
+    p.nh = a.n_heads;
+    p.nkv = a.n_kv_heads;
+    p.hd = a.head_dim;
+    p.cols = (a.n_heads + 2 * a.n_kv_heads) * a.head_dim;
+    p.x_cb = !f32 && a.x_layout == SL_LAYOUT_T16X32 ? (p.cols + 31) / 32 : 0;
+    p.q_cb = a.q_layout == SL_LAYOUT_T16X32 ? (a.n_heads * a.head_dim + 31) / 32 : 0;
+    p.half = a.rope_kind != SL_ROPE_NONE ? a.rope_dim / 2 : 0;
+    p.split = a.rope_kind == SL_ROPE_HALF;
+    p.rope_factor = a.rope_factor;
+    const auto factor = [&](float scale) { return f32 ? 1.0f / scale : (float)((double)a.x_scale / scale); };
+    p.fq = factor(a.q_scale);
+    p.fk = factor(a.k_scale);
+    p.fv = factor(a.v_scale);
+    const int32_t width = vec ? 8 : 2;
+    p.q_columns = a.q ? a.n_heads * (a.head_dim / width) : 0;
+    p.k_columns = a.n_kv_heads * (a.head_dim / width);
+    p.v_columns = a.n_kv_heads * (a.head_dim / 4);
+    p.inv_qk = (float)width / a.head_dim;
+    p.inv_value = 4.0f / a.head_dim;
+    p.inv_half = p.half ? 1.0f / p.half : 0.0f;
+    const bool step = a.max_new == 1;
     constexpr int32_t kMostGrid = 65535;  // workgroups of a launch in its second and third dimension
     // (the first may begin anywhere in 16 slots; a launch of fewer goes through them in turns)
-    const int64_t groups = step ? 1 : std::min<int64_t>(((int64_t)args.max_new + 30) / 16, kMostGrid);
-    // Features over several workgroups: in a step a column a thread, else until there are enough to fill the CUs.
-    const double tokens = std::min((double)groups * args.n_seq, (double)args.m_tokens / 16 + args.n_seq);
-    int32_t parts = (p.columns + 255) / 256;
-    if (!step) parts = (int32_t)std::max(1.0, std::min((p.columns + kColumns - 1) / kColumns + 0.0, APARTS / tokens));
-    p.per = (p.columns + parts - 1) / parts;
-    if (!step) p.per = (p.per + kColumns - 1) / kColumns * kColumns;
-    parts = (p.columns + p.per - 1) / p.per;
-    if ((double)groups * args.n_seq * parts > 0x7fffffff / (4 * kColumns)) {
+    const int64_t groups = step ? 1 : std::min<int64_t>(((int64_t)a.max_new + 30) / 16, kMostGrid);
+    // Columns of a workgroup: in a step one a thread; else as few as leave work for all CUs, since each of them computes
+    // its tokens' angles again.
+    const auto even = [](int32_t columns, int32_t most) {  // in equal parts of at most so many
+        const int32_t parts = std::max((columns + most - 1) / most, 1);
+        return std::max((columns + parts - 1) / parts, 1);
+    };
+    const double tokens = std::min((double)groups * a.n_seq, (double)a.m_tokens / 16 + a.n_seq);
+    int32_t most = 256;
+    if (!step)
+        while (most > 64 && tokens * (p.q_columns + p.k_columns + p.v_columns) / most < 4096) most /= 2;
+    p.per = even(std::max(p.q_columns, p.k_columns), most);
+    p.v_per = even(p.v_columns, most);
+    p.q_parts = (p.q_columns + p.per - 1) / p.per;
+    p.k_parts = (p.k_columns + p.per - 1) / p.per;
+    const int32_t parts = p.q_parts + p.k_parts + (p.v_columns + p.v_per - 1) / p.v_per;
+    if ((double)groups * a.n_seq * parts > 0x7fffffff / 256) {
         set_error("too many work items for one launch");
         return SL_ERR_UNSUPPORTED;
     }
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    for (int64_t s0 = 0; s0 < args.n_seq; s0 += kMostGrid) {
+    for (int64_t s0 = 0; s0 < a.n_seq; s0 += kMostGrid) {
         p.seq0 = (int32_t)s0;
-        const dim3 grid((uint32_t)parts, (uint32_t)groups, (uint32_t)std::min(args.n_seq - p.seq0, kMostGrid));
-        const auto run = [&](auto types, auto width) {
-            constexpr bool F = decltype(types)::value, V = decltype(width)::value;
+        const dim3 grid((uint32_t)parts, (uint32_t)groups, (uint32_t)std::min(a.n_seq - p.seq0, kMostGrid));
+        const auto run = [&](auto types, auto widths) {
+            constexpr bool F = decltype(types)::value, V = decltype(widths)::value;
             if (step)
                 hipLaunchKernelGGL((cache_append_step_kernel<F, V>), grid, dim3(256), 0, s, p);
             else
-                hipLaunchKernelGGL((cache_append_kernel<F, V>), grid, dim3(4 * kColumns), 0, s, p);
+                hipLaunchKernelGGL((cache_append_kernel<F, V>), grid, dim3(256), 0, s, p);
         };
         if (f32 && vec)
             run(std::true_type{}, std::true_type{});
