@@ -616,11 +616,14 @@ __global__ __launch_bounds__(256) void cache_join_kernel(const CacheArgs a)
     const int tid = threadIdx.x;
     const int32_t seq = a.seq0 + blockIdx.y;
     const int32_t kv = a.tiles == 1 ? blockIdx.x : blockIdx.x / (uint32_t)a.tiles, tile = blockIdx.x - kv * a.tiles;
-    const Tokens tk = tokens_of(a.seq_start, seq, a.m);
+    int32_t b0 = ((ScalarTable)(uintptr_t)a.seq_start)[seq], b1 = ((ScalarTable)(uintptr_t)a.seq_start)[seq + 1];
+    int32_t len = ((ScalarTable)(uintptr_t)a.kv_len)[seq];
+    asm volatile("" : "+s"(b0), "+s"(b1), "+s"(len));  // (here they are all waited for, instead of one after the other)
+    const Tokens tk = tokens_between(b0, b1, a.m);
     const int64_t first_row = (int64_t)tile * a.tile_rows;
     const int64_t rows = min((int64_t)tk.n * a.group - first_row, (int64_t)a.tile_rows);
     if (rows <= 0) return;
-    const int32_t len = max(a.kv_len[seq], 0);
+    len = max(len, 0);
     const int32_t cached = (int32_t)min((int64_t)len, (int64_t)a.max_pages << a.shift);
     const int32_t most = a.causal ? min(len - tk.n + (int32_t)by_group(a, first_row + rows - 1) + 1, cached) : cached;
     const int32_t n = min(a.splits, max(1, (most + a.split_keys - 1) / a.split_keys));

@@ -40,10 +40,10 @@ void cache_prompt_kernel(const CacheArgs a)
     const int lane = threadIdx.x & 63, half = lane >> 5, n32 = lane & 31;
     const int number = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = number % RW, part = number / RW;
     char *lds = all_lds + part * 2 * BUF;
-    // tiles of a sequence from the last, which sees the most keys, for all heads and sequences
+    // every sequence's last tile, which sees its most keys, then the ones before them: the longest work begins first
     const int32_t kv = blockIdx.x, seq = a.seq0 + blockIdx.y;
     const int32_t from_last = a.splits == 1 ? blockIdx.z : blockIdx.z / (uint32_t)a.splits;
-    const int32_t tile0 = a.tiles - 1 - from_last, split = blockIdx.z - from_last * a.splits;
+    const int32_t split = blockIdx.z - from_last * a.splits;
     // (without pages nothing is taken from it; the read has to be somewhere)
     const int32_t *row_of_table = a.max_pages ? a.page_table + (int64_t)seq * a.max_pages : a.kv_len;
     const ScalarTable table = (ScalarTable)(uintptr_t)row_of_table;
@@ -138,7 +138,8 @@ void cache_prompt_kernel(const CacheArgs a)
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     };
 
-    for (int64_t tile = tile0; tile * TQ < rows; tile += a.tiles) {
+    const int64_t tile0 = (rows + TQ - 1) / TQ - 1 - from_last;
+    for (int64_t tile = tile0; tile >= 0; tile -= a.tiles) {
         const int64_t first_row = tile * TQ, end_row = min(first_row + TQ, rows);
         const int32_t i0 = (int32_t)by_group(a, first_row), g0 = (int32_t)(first_row - (int64_t)i0 * a.group);
         // a lane's query: token, or -1, and head
@@ -358,7 +359,7 @@ void cache_prompt_kernel(const CacheArgs a)
                             o[d][e] = o[d][e] * f + to[(k * RW + wave) * (1024 * N) + 64 * (16 * d + e)] * f2;
                 }
             }
-            if ((tile + a.tiles) * TQ < rows) __syncthreads();  // (before the next tile's keys come)
+            if (tile >= a.tiles) __syncthreads();  // (before the next tile's keys come)
             if (part) continue;
         }
         const int32_t i = query(head);
