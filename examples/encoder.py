@@ -28,19 +28,20 @@ LINEARS = ("qkv", "out", "ffn1", "ffn2")
 
 
 class Layer:
-    """Weights of one layer, dense on the host and packed on the device, and its two norms."""
+    """Weights of one layer, dense on the host and packed on the device, and its norms (an encoder's: two)."""
 
-    def __init__(self, hidden, inter, sparsity, seed):
+    def __init__(self, hidden, inter, sparsity, seed, shapes=None, norms=2):
         self.dense, self.packed = {}, {}
-        shapes = {"qkv": (3 * hidden, hidden), "out": (hidden, hidden), "ffn1": (inter, hidden), "ffn2": (hidden, inter)}
+        shapes = shapes or {"qkv": (3 * hidden, hidden), "out": (hidden, hidden), "ffn1": (inter, hidden),
+                            "ffn2": (hidden, inter)}
         for op, (name, (n, k)) in enumerate(shapes.items()):
             d = make_weight(n, k, sparsity, seed=seed, op=op)
             d["sw"] = np.full(n, 1.5 / (73 * math.sqrt(k * (1 - sparsity))), np.float32)  # outputs of about x's size
             self.dense[name] = d
             self.packed[name] = sl.PackedWeight.pack(d["w"], d["sw"], d["b"])
         g = torch.Generator(device="cuda").manual_seed(seed)
-        self.gamma = [1 + 0.1 * torch.randn(hidden, device="cuda", generator=g) for _ in range(2)]
-        self.beta = [0.05 * torch.randn(hidden, device="cuda", generator=g) for _ in range(2)]
+        self.gamma = [1 + 0.1 * torch.randn(hidden, device="cuda", generator=g) for _ in range(norms)]
+        self.beta = [0.05 * torch.randn(hidden, device="cuda", generator=g) for _ in range(norms)]
 
     def plain(self, name, x):
         d = self.dense[name]
