@@ -698,9 +698,10 @@ def cache_attention(q, cache, page_table, seq_start, kv_len, max_new: int, max_l
         out = torch.empty_like(q) if dt is torch.int8 and q.shape == shape else torch.empty(shape, dtype=dt, device=q.device)
     elif out.dtype is not dt or out.shape != shape or not out.is_contiguous() or out.device != q.device:
         raise ValueError("out has the wrong dtype/shape/device or is not contiguous")
-    scale = head_dim ** -0.5 if softmax_scale is None and head_dim else softmax_scale
+    if softmax_scale is None:
+        softmax_scale = head_dim ** -0.5 if head_dim else 1.0  # (no head: refused below)
     fields = (n_seq, max_new, max_len, pages, n_pages, page_size, q_layout, q_cols, n_heads, n_kv, head_dim,
-              1 if causal else 0, kind, y_layout, q_scale, k_scale, v_scale, scale, out_scale)
+              1 if causal else 0, kind, y_layout, q_scale, k_scale, v_scale, softmax_scale, out_scale)
     head = (q.data_ptr(), m_tokens, seq_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), cache.data_ptr(),
             out.data_ptr())
     lib, args = load(), _CACHE_ARGS.pack(*head, 0, 0, *fields)

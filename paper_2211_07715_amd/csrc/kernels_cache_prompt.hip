@@ -80,7 +80,7 @@ void cache_prompt_kernel(const CacheArgs a)
 
     // A lane's pieces of its wave's 16 tokens: bytes from the first one's, and where they go. Row 8 i + 4 h + b of 16 is
     // key 8 h + 4 i + b, as a lane half h of the scores has them.
-    uint32_t koff[KP], voff[VP], vdst[VP];
+    uint32_t koff[KP], vdst[VP];
     bool kmine[KP], vmine[VP];
 #pragma unroll
     for (int i = 0; i < KP; ++i) {
@@ -93,7 +93,6 @@ void cache_prompt_kernel(const CacheArgs a)
     for (int i = 0; i < VP; ++i) {
         const int d = lane + 64 * i;
         vmine[i] = d < a.hd;
-        voff[i] = (uint32_t)d * 16;
         // (lane half h of the product's rows 8 x + 4 h + b then holds features 16 N h + 16 tile + 4 x + b)
         const int row = 32 * (d / 16 % N) + 8 * (d / 4 % 4) + 4 * (d / (16 * N)) + d % 4;
         vdst[i] = KB + row * VS + 16 * vswap(row);
@@ -111,7 +110,7 @@ void cache_prompt_kernel(const CacheArgs a)
                 if (kmine[i]) load_to_lds(k, buf + group * 16 * KS + 1024 * i, koff[i], 0);
 #pragma unroll
             for (int i = 0; i < VP; ++i)
-                if (vmine[i]) vreg[g][i] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(v, voff[i], 0, 0));
+                if (vmine[i]) vreg[g][i] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(v, 16 * here(lane), 1024 * i, 0));
         }
     };
     const auto stage = [&](char *buf) __attribute__((always_inline)) {

@@ -286,6 +286,14 @@ def test_attention_more_than_said(hip, new):
     run_attend(hip, rng, b, 4)
 
 
+@pytest.mark.parametrize("nh,nkv", [(16, 1), (17, 1), (40, 2), (100, 1)])
+@pytest.mark.parametrize("news,lens", [([1, 1], [600, 33]), ([3, 20], [30, 700])])
+def test_attention_large_groups(hip, nh, nkv, news, lens):
+    """More query heads a key head than a tile has rows."""
+    rng = np.random.default_rng(nh)
+    run_attend(hip, rng, Batch(hip, rng, news, lens, 32, nkv, 32), nh)
+
+
 def test_attention_many_sequences(hip):
     rng = np.random.default_rng(17)
     lens = [int(n) for n in rng.integers(0, 90, 700)]

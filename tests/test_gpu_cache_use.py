@@ -267,6 +267,10 @@ def test_what_the_binding_refuses(hip):
         append(hip, x, b, 4, rope=hip.ROPE_HALF, inv_freq=torch.ones(33, device="cuda"))  # more than half a head
     with pytest.raises(hip.SparseLinearError):
         attend(hip, q, b, 4, softmax_scale=-1.0)
+    with pytest.raises(hip.SparseLinearError):  # heads of no features
+        b.dev = [good[0][..., :0].contiguous(), *good[1:]]
+        attend(hip, q, b, 4)
+    b.dev = good
 
 
 def test_nothing_to_do(hip):
