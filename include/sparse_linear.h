@@ -462,9 +462,9 @@ sl_status cache_append(const sl_cache_append_args *args, void *hip_stream);
  *   workspace   cache_attention_workspace(args) bytes (0: may be NULL), 16-byte
  *               aligned, held until the stream has passed the call; calls that may
  *               run at the same time each have their own
- * Other fields as in cache_append. Softmax weights enter the products as 23-bit
- * parts of a span's largest (spans of up to 128 keys), or, for many queries, as
- * in attention_run. Results do not depend on timing.
+ * Other fields as in cache_append. Softmax weights enter the products with 23 bits
+ * of the largest of 64 keys, or, for many queries, as in attention_run. Results do
+ * not depend on timing.
  * Errors: SL_ERR_INVALID_ARG, SL_ERR_SHAPE (sizes), SL_ERR_UNSUPPORTED (more
  * work items than a launch takes).
  */
@@ -546,14 +546,16 @@ int32_t sl_abi_version(void);
 
 /*
  * Thread-local text naming the kernel and workgroup shape of the last
- * successful sparse_linear_run / sparse_linear_run_layout / attention_run that
- * launched one on this thread ("" before the first): "split st,nt kw=K wpw=W" (split reduction, for
+ * successful sparse_linear_run / sparse_linear_run_layout / attention_run /
+ * cache_attention that launched one on this thread ("" before the first): "split st,nt kw=K wpw=W" (split reduction, for
  * few tokens), "panel nt,st,nwv,r" (weight-stationary), "tile tokens,nt" (long
  * reductions), "direct st,nt,wm,d" or "staged st,ct,wm,wn,d", followed by " gelu=erf" when an
  * int8 GELU epilogue evaluated erf because its output scale (below about
  * 0.015) admits no step table; "attention features,tiles,waves,split" (features
  * that a head is padded to, tiles of 32 queries a wave, waves that share a chunk
- * of keys, parts that the keys are split into), followed by " lists" with blocks.
+ * of keys, parts that the keys are split into), followed by " lists" with blocks;
+ * "cache split features,parts" or "cache prompt features,parts" (kernels for few and
+ * for many queries, features of a head, parts that the keys are split into).
  * For tests and tuning; the text is valid until
  * the next run on this thread.
  */

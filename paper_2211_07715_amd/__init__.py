@@ -326,7 +326,7 @@ class PackedWeight:
 
 
 def last_path() -> str:
-    """Kernel and workgroup shape of the last successful run (of a linear or of attention) on this thread."""
+    """Kernel and workgroup shape of the last successful run (of a linear or of either attention) on this thread."""
     return load().sl_last_path().decode()
 
 

@@ -1,4 +1,42 @@
-// cache_append and cache_attention for few queries a sequence (gfx950).
+// A decoder's cache (gfx950): cache_append, and cache_attention for few queries a
+// sequence. (kernels_cache_prompt.hip has it for many.)
+//
+// cache_append. Memory bounds it: an element is read once (4 bytes or 1), turned by
+// 4 operations and written as one byte. A token's angles serve all its heads, so a
+// workgroup computes them once in LDS (position times frequency in 64 bits, reduced
+// to quarter turns) and goes through its columns. 16 slots go together, because a
+// page holds 16 tokens' codes of a value's feature in 16 bytes; with one token a
+// sequence these are single bytes, 16 apart. What a wave's lanes have in common, its
+// token, and what its tokens have in common, a lane's features, make up an address,
+// so that neither loads nor stores compute one.
+//   Measured, replayed from a graph: 4 x 4096 tokens of 32 heads of 128 that 4 share,
+// fp32, 97.5 us (5.16 TB/s; a copy of 1 GiB reaches 5.20), from int8 codes 53 (3.8
+// TB/s; vector instructions: 8 an element); 24 ragged prompts of up to 384 tokens of
+// 12 heads of 64, int8, 16.5 us; 64 sequences of one token, fp32, 4.3 us, one 3.2 us.
+//
+// cache_attention, few queries: each key and value byte is read once, for 4
+// operations and query head that shares it, so memory bounds it. Nothing passes
+// through LDS on the way to the matrix instructions: keys and values lie in a page
+// as lanes take them (16 bytes are 16 features of a key, or 16 tokens of a feature).
+//   S = K Q^T     int8 x int8 -> int32 on v_mfma_i32_16x16x64_i8, exact
+//   P = 2^(c (S - m)), m the largest of a span of 64 keys: as whole numbers of 23
+//       bits in three signed bytes
+//   O += V^T P^T  int8 x int8 -> int32, exact, a product for each byte
+// Values need no conversion, sums of a span are whole numbers, and a span's results
+// join the others' in fp32 by their m. Row x of a score tile is the key that makes a
+// lane's scores those of the 16 tokens whose values it takes, so weights stay in
+// their lane. A column is a (query, head) pair: heads that share keys share the rows.
+//   A wave takes every 4th span of 64 keys. Three waves a SIMD, whose loads are all
+// under way before a span's first product, keep memory busy: asking for the next
+// span during the products of one took registers for two waves and gave the same
+// rate; spans of 128 keys gave the same (99.6 us) and cost short sequences (5.4
+// against 4.7 us).
+//   Measured, replayed from a graph: 64 x 4096 tokens of 8 key heads of 128 with 4
+// query heads each 99 us (5.4 TB/s; reading alone reaches 6.4), 64 x 16384 376 (5.7),
+// 131072 tokens 57 to 61 (50 and 5 for the two launches), 24 ragged sequences of up
+// to 3001 tokens of 8 heads of 96 18.9 (2.7 TB/s: 17 and 4), 32 x 384 tokens of 12
+// heads of 64 8.7, 128 tokens 4.7. Vector instructions are active 30 % of the time
+// in the first, matrix ones 7 %.
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -66,6 +104,16 @@ __device__ __forceinline__ uint32_t feature_offset(int32_t c, int32_t cb, int32_
     return cb ? (uint32_t)(c >> 5) * 512 + (c & 31) : (uint32_t)c * size;
 }
 
+// number / by and what is left of it; number is under 2^23 and its quotient in fp32 off by less than one.
+__device__ __forceinline__ void divide(int32_t number, int32_t by, float inv, int32_t &quotient, int32_t &rest)
+{
+    quotient = (int32_t)(((float)number + 0.5f) * inv);
+    rest = number - quotient * by;
+    const int32_t more = rest < 0 ? -1 : rest >= by ? 1 : 0;
+    quotient += more;
+    rest -= more * by;
+}
+
 // What a thread does: a column, which is 8 features of a query or key head (VEC:
 // rope_dim is a multiple of 8, so that 4 features of both halves of pairs lie
 // together; else 2 features), or 4 features of a value head. A workgroup's columns
@@ -79,8 +127,8 @@ struct PairColumn {
     uint32_t x0, x1, d0, d1;  // bytes of both parts from a token's first: in x, and where their codes go
     __device__ __forceinline__ PairColumn(const AppendArgs &p, int32_t number, bool keys)
     {
-        // (number / columns of a head: under 2^23, and half a column from every whole number of heads)
-        const int32_t head = (int32_t)(((float)number + 0.5f) * p.inv_qk), k = number - head * (p.hd / U);
+        int32_t head, k;
+        divide(number, p.hd / U, p.inv_qk, head, k);
         w0 = VEC ? 4 * k : k;
         turned = w0 < p.half;
         const bool apart = turned && p.split;
@@ -139,7 +187,9 @@ struct ValueColumn {
     uint32_t x0, d0;  // bytes from a token's first in x, and from a page's first value in a group of 16 tokens
     __device__ __forceinline__ ValueColumn(const AppendArgs &p, int32_t number)
     {
-        const int32_t head = (int32_t)(((float)number + 0.5f) * p.inv_value), c = 4 * (number - head * (p.hd / 4));
+        int32_t head, c;
+        divide(number, p.hd / 4, p.inv_value, head, c);
+        c *= 4;
         x0 = feature_offset((p.nh + p.nkv + head) * p.hd + c, p.x_cb, F32 ? 4 : 1);
         d0 = (uint32_t)(head << p.shift) * p.hd + c * 16;
     }
@@ -700,13 +750,26 @@ Plan plan_of(const sl_cache_attention_args &a)
     const auto items_of = [&](int32_t tile_rows) {  // (a product of whole numbers may not fit)
         return (double)a.n_seq * a.n_kv_heads * (double)((rows + tile_rows - 1) / tile_rows);
     };
+    // Tiles of 16 rows with the keys split as far as it takes, against 64 or 128 rows that share a chunk of keys (12 heads
+    // of 64): 48 queries over 8192 keys (36 tiles of 16 rows) 15 us against 20, 8 times 48 over 2048 (288) 22 against 26,
+    // 512 over 8192 (384) 42 against 42, 32 times 128 over 384 (3072) 28 against 17; 8 heads of 128 that 4 share, 8 times 64
+    // over 4096 (1024) 101 against 77.
     Plan p{rows > 16 && items_of(16) > 384, 16, 1, 0, 0};
     if (p.prompt) {
-        // (m_tokens bounds what sequences of different lengths have together: half a tile more each)
+        // 64 rows, which two waves on either half of the chunks have, against 128 in four waves, where a workgroup has few
+        // chunks or there are few (12 heads of 64): one of 2048 tokens (192 tiles of 128) 30 us against 36, 16 ragged ones
+        // (about 440) 46 against 61, 32 times 128 over 384 (384) 16.9 against 19.1; 4 times 2048 (768) 58 against 55, 32
+        // times 512 (1536) 46 against 38. (m_tokens bounds what sequences of different lengths have together: half a tile
+        // more each.) Wider heads have no room for two sets of chunks.
         const double real = (double)a.n_kv_heads * ((double)a.m_tokens * group / 128 + 0.5 * a.n_seq);
-        p.tile_rows = a.head_dim <= 64 && std::min(items_of(128), real) < 512 ? 64 : 128;
+        p.tile_rows = a.head_dim <= 64 && (rows <= 64 || std::min(items_of(128), real) < 512) ? 64 : 128;
     }
     p.tiles = (rows + p.tile_rows - 1) / p.tile_rows;
+    // Keys in parts, where there are too few tiles for the CUs and enough keys to pay for joining them (4 us and more): one
+    // query over 131072 keys of 8 heads of 128 in 64 parts 58 us, in 32 58, in 128 61, in one 873; 16 queries over 4096 in 4
+    // 35, in one 40; 32 over 384 keys of 12 heads (384 tiles) in one 8.9, in 2 12.0. Of 128 rows: 8 times 64 over 4096 keys
+    // of 8 heads of 128 that 4 share (128 tiles) in 3 77, in 6 85, in one 114; 64 times 16 over 1024 (512) in one 47, in
+    // 2 69.
     const double all = items_of(p.tile_rows);
     const int32_t enough = p.prompt ? 384 : 512, least = p.prompt ? 1024 : 512;
     if (all >= enough) return p;
@@ -776,8 +839,9 @@ sl_status launch_cache_append(const sl_cache_append_args &a, void *stream)
     constexpr int32_t kMostGrid = 65535;  // workgroups of a launch in its second and third dimension
     // (the first may begin anywhere in 16 slots; a launch of fewer goes through them in turns)
     const int64_t groups = step ? 1 : std::min<int64_t>(((int64_t)a.max_new + 30) / 16, kMostGrid);
-    // Columns of a workgroup: in a step one a thread; else as few as leave work for all CUs, since each of them computes
-    // its tokens' angles again.
+    // Columns of a workgroup: in a step one a thread; else as many as leave 4096 workgroups, since each of them computes
+    // its tokens' angles (4 x 4096 tokens of 32 heads of 128 that 4 share: 99.5 us from fp32 and 54 from int8; with 1024
+    // 105.8 and 52, with 16384 98 and 73; ragged prompts, which have fewer in all, 17.7 to 17.8).
     const auto even = [](int32_t columns, int32_t most) {  // in equal parts of at most so many
         const int32_t parts = std::max((columns + most - 1) / most, 1);
         return std::max((columns + parts - 1) / parts, 1);
