@@ -348,7 +348,11 @@ void cache_prompt_kernel(const CacheArgs a)
                 const float sum = weights(sc);
                 if (__any(!(sum < kMostSum))) break;  // (no weight is over 65504 while their sum is below that)
                 l += sum;
+                // (matrix instructions of one wave before vector ones of another: 4096 tokens of 32 heads of 128 on 8 199 us
+                // against 210, 8192 of 16 of 64 on 4 227 against 232)
+                __builtin_amdgcn_s_setprio(1);
                 multiply(lds + buf);
+                __builtin_amdgcn_s_setprio(0);
                 advance();
             }
         }
