@@ -8,7 +8,7 @@ Bars.
 - Attention: the weights' relative error is that of the exponential's argument x <= 24 that matters, |x| 2^-23 ln 2 (its
   factor's and its product's rounding), weighted with 2^-x under 1e-7 of the largest, over many keys of which each
   weighs little at most 24 * 2^-23 * ln 2 = 2e-6; the instruction's own 2^-22; and the whole number that stands for a
-  weight, 2^-24 of its span's largest, which 128 keys of a span that rounds one way could add up to 2^-17 (the sum of
+  weight, 2^-24 of its span's largest, which the up to 128 keys of a span, all rounded one way, could add up to 2^-17 (the sum of
   weights moves with it). Sums in 32 bits: 2^-24 for each of up to 100 additions, 6e-6. Together under 2e-5 of the
   largest |v| = 127 v_scale, for the numerator and again for the denominator: TOL = 4e-5 * 127 v_scale.
 """
