@@ -580,27 +580,25 @@ def cache_shape(n_pages: int, page_size: int, n_kv_heads: int, head_dim: int):
 
 
 def _cache_args(x, name, cache, page_table, seq_start, kv_len, stream):
-    """Checks of what cache_append and cache_attention share; returns (n_seq, pages of a sequence, the stream's number).
-    The launch goes to the current device, so the tensors (and the stream) have to be there."""
+    """Checks of what cache_append and cache_attention share; returns (n_seq, pages of a sequence, the cache's shape, the
+    stream's number). The launch goes to the current device, so the tensors (and the stream) have to be there."""
     torch = _torch or _torch_once()
-    dev, i32 = x.get_device(), torch.int32
+    dev, i32, shape, table = x.get_device(), torch.int32, cache.shape, page_table.shape
     if dev < 0 or not x.is_contiguous():
         raise ValueError(f"{name} must be a contiguous CUDA tensor")
-    if cache.dtype is not torch.int8 or cache.dim() != 5 or cache.shape[1] != 2 or not cache.is_contiguous():
+    if cache.dtype is not torch.int8 or len(shape) != 5 or shape[1] != 2 or not cache.is_contiguous():
         raise ValueError("cache must be a contiguous int8 tensor of cache_shape()")
-    if page_table.dtype is not i32 or page_table.dim() != 2 or not page_table.is_contiguous():
+    if page_table.dtype is not i32 or len(table) != 2 or not page_table.is_contiguous():
         raise ValueError("page_table must be a contiguous int32 tensor [n_seq, pages]")
-    if seq_start.dtype is not i32 or seq_start.dim() != 1 or not seq_start.is_contiguous() or \
-            kv_len.dtype is not i32 or kv_len.dim() != 1 or not kv_len.is_contiguous():
-        raise ValueError("seq_start and kv_len must be contiguous 1-D int32 tensors")
-    n_seq, pages = page_table.shape
-    if len(kv_len) != n_seq or len(seq_start) != n_seq + 1:
-        raise ValueError("seq_start has n_seq + 1 entries, kv_len and page_table n_seq")
+    n_seq, pages = table
+    if seq_start.dtype is not i32 or kv_len.dtype is not i32 or kv_len.shape != (n_seq,) or \
+            seq_start.shape != (n_seq + 1,) or not seq_start.is_contiguous() or not kv_len.is_contiguous():
+        raise ValueError("seq_start and kv_len must be contiguous int32 tensors [n_seq + 1] and [n_seq], as page_table's")
     if not (cache.get_device() == page_table.get_device() == seq_start.get_device() == kv_len.get_device() == dev):
         raise ValueError(f"cache, page_table, seq_start and kv_len must be on {name}'s device")
     if torch._C._cuda_getDevice() != dev or (stream is not None and stream.device_index != dev):
         raise ValueError("the tensors' device must be the current one, and the stream's")
-    return n_seq, pages, _stream_ptr(stream)
+    return n_seq, pages, shape, _stream_ptr(stream)
 
 
 def cache_append(x, cache, page_table, seq_start, kv_len, max_new: int, n_heads: int, *, x_scale: float = 1.0,
@@ -618,8 +616,8 @@ def cache_append(x, cache, page_table, seq_start, kv_len, max_new: int, n_heads:
     encoder's keys and values). Returns the query codes [M, n_heads * head_dim] in q_layout, or None without q_scale.
     Tokens of no sequence are left as they are."""
     torch = _torch or _torch_once()
-    n_seq, pages, s = _cache_args(x, "x", cache, page_table, seq_start, kv_len, stream)
-    n_pages, _, n_kv, page_size, head_dim = cache.shape
+    n_seq, pages, (n_pages, _, n_kv, page_size, head_dim), s = _cache_args(x, "x", cache, page_table, seq_start, kv_len,
+                                                                           stream)
     cols = (n_heads + 2 * n_kv) * head_dim
     x_type = ACT_F32 if x.dtype is torch.float32 else ACT_I8
     if x_type == ACT_I8 and x.dtype is not torch.int8:
@@ -676,8 +674,8 @@ def cache_attention(q, cache, page_table, seq_start, kv_len, max_new: int, max_l
     1 / sqrt(head_dim). Returns [M, n_heads * head_dim]: int8 codes of out_scale (EPI_I8, y_layout) or fp32 (EPI_F32); 0
     where nothing is seen. Tokens of no sequence are left as they are."""
     torch = _torch or _torch_once()
-    n_seq, pages, s = _cache_args(q, "q", cache, page_table, seq_start, kv_len, stream)
-    n_pages, _, n_kv, page_size, head_dim = cache.shape
+    n_seq, pages, (n_pages, _, n_kv, page_size, head_dim), s = _cache_args(q, "q", cache, page_table, seq_start, kv_len,
+                                                                           stream)
     if q.dtype is not torch.int8:
         raise ValueError("q must be int8")
     cols = n_heads * head_dim

@@ -41,6 +41,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <charconv>
 #include <type_traits>
 
 #include "cache_device.h"
@@ -752,8 +753,8 @@ Plan plan_of(const sl_cache_attention_args &a)
     };
     // Tiles of 16 rows with the keys split as far as it takes, against 64 or 128 rows that share a chunk of keys (12 heads
     // of 64): 48 queries over 8192 keys (36 tiles of 16 rows) 15 us against 20, 8 times 48 over 2048 (288) 22 against 26,
-    // 512 over 8192 (384) 42 against 42, 32 times 128 over 384 (3072) 28 against 17; 8 heads of 128 that 4 share, 8 times 64
-    // over 4096 (1024) 101 against 77.
+    // 512 over 8192 (384) 42 against 42, 32 times 128 over 384 (eight times as many) 28 against 17; 8 heads of 128 that 4
+    // share, 8 times 64 over 4096 (1024) 101 against 77.
     Plan p{rows > 16 && items_of(16) > 384, 16, 1, 0, 0};
     if (p.prompt) {
         // 64 rows, which two waves on either half of the chunks have, against 128 in four waves, where a workgroup has few
@@ -955,7 +956,14 @@ sl_status launch_cache_attention(const sl_cache_attention_args &args, void *stre
             HIP_TRY(hipGetLastError());
         }
     }
-    set_last_path("cache %s %d,%d", p.prompt ? "prompt" : "split", a.hd, a.splits);
+    // (numbers put down by hand: formatting them is a part of what a short call costs)
+    char name[40] = "";
+    char *end = name + sizeof(name) - 1, *at = name;
+    for (const char *c = p.prompt ? "cache prompt " : "cache split "; *c; ++c) *at++ = *c;
+    at = std::to_chars(at, end, a.hd).ptr;
+    *at++ = ',';
+    *std::to_chars(at, end, a.splits).ptr = 0;
+    set_last_path("%s", name);
     return SL_OK;
 }
 
