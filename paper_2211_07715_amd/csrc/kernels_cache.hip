@@ -677,7 +677,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(const CacheArgs a)
     len = max(len, 0);
     const int32_t cached = (int32_t)min((int64_t)len, (int64_t)a.max_pages << a.shift);
     const int32_t most = a.causal ? min(len - tk.n + (int32_t)by_group(a, first_row + rows - 1) + 1, cached) : cached;
-    const int32_t n = min(a.splits, max(1, (most + a.split_keys - 1) / a.split_keys));
+    const int32_t n = min(a.splits, (max(most, 1) - 1) / a.split_keys + 1);  // (a part's keys more may not fit)
     const float *rec = a.work + (((int64_t)seq * a.n_kv + kv) * a.tiles + tile) * a.splits * record(a.hd, a.tile_rows);
     const int quads = a.hd / 4, per = quads * a.join_group, here_rows = 256 / per;  // rows of a workgroup at a time
     const int mine = tid / per, group = tid % per / quads, c = tid % quads * 4;

@@ -167,6 +167,33 @@ def test_a_cache_past_32_bit_offsets(hip):
     assert not cache[:base].any()
 
 
+def test_the_longest_sequence(hip):
+    """As many tokens as a table may name, 2^31 - 65536: its first half all in one page, its second in another. (A wave adds
+    up 2^31 / (512 parts * 4 waves * 64 keys) = 16384 spans, and a query's join under 200 parts: 2^-24 of the sum for each
+    addition, in the numerator and in the denominator, is 2e-3 of the largest |v|.)"""
+    import torch
+    rng = np.random.default_rng(12)
+    ps, hd, entries = 256, 16, 2 ** 23 - 256
+    cache = codes(rng, *hip.cache_shape(2, ps, 1, hd))
+    values = cache[:, 1, 0].reshape(2, ps // 16, hd, 16)  # (a view)
+    values[0], values[1] = np.abs(values[0]), -np.abs(values[1])
+    q = codes(rng, 1, hd)
+    table = torch.zeros((1, entries), dtype=torch.int32, device="cuda")
+    table[:, entries // 2:] = 1
+    length = entries * ps
+    y = hip.cache_attention(cuda(q), cuda(cache), table, cuda(np.array([0, 1], np.int32)), cuda(np.array([length], np.int32)),
+                            1, length, 1, q_scale=0.04, k_scale=0.05, v_scale=0.03, kind=hip.EPI_F32)
+    assert hip.last_path() == "cache split 16,512"
+    z = cache[:, 0, 0].astype(np.float64) @ q[0] * (float(np.float32(0.04)) * float(np.float32(0.05)) / 4)
+    w = np.exp(z - z.max())  # [2, ps], each key as often as any other
+    v = values.astype(np.float64).transpose(0, 1, 3, 2).reshape(2, ps, hd)
+    want = (w[..., None] * v).sum((0, 1)) / w.sum() * float(np.float32(0.03))
+    bar = (2e-3 * 127 + TOL) * 0.03
+    first = (w[0, :, None] * v[0]).sum(0) / w[0].sum() * 0.03
+    assert np.abs(first - want).max() > 2 * bar
+    assert np.abs(y.cpu().numpy() - want).max() <= bar
+
+
 def test_activations_past_32_bit_offsets(hip):
     """The tokens of the last sequence lie beyond 4 GiB of fp32 x; only they belong to one."""
     import torch
