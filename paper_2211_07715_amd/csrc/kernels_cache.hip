@@ -489,10 +489,11 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(3))
         const bool real = tile * 16 + r < rows;
         const int32_t di = a.group >= 16 ? (g0 >= a.group ? 1 : 0) : (int32_t)(((float)g0 + 0.5f) * a.inv_group);  // (g0 < 32)
         const int32_t i = i0 + di, head = kv * a.group + (g0 - di * a.group);
-        const int32_t limit = !real ? 0 : a.causal ? min(len - tk.n + i + 1, cached) : cached;
-        // (a tile's queries see no more keys than its last one, lane 15's or the last real one's)
+        // (a tile's queries see no more keys than its last one, lane 15's or the last real one's; lanes without a query see
+        // as many, so that spans seen whole need no masks)
         const int32_t last = min(__builtin_amdgcn_readlane(i, 15), tk.n - 1);
         const int32_t most = a.causal ? min(len - tk.n + last + 1, cached) : cached;
+        const int32_t limit = real && a.causal ? min(len - tk.n + i + 1, cached) : most;
         const int32_t k0 = whole ? 0 : split * a.split_keys;
         const int32_t k1 = whole || split == a.splits - 1 ? most : min(most, k0 + a.split_keys);
         if (!whole && k0 >= most && split) continue;  // (part 0 says that there is none)
