@@ -10,9 +10,9 @@
 // token, and what its tokens have in common, a lane's features, make up an address,
 // so that neither loads nor stores compute one.
 //   Measured, replayed from a graph: 4 x 4096 tokens of 32 heads of 128 that 4 share,
-// fp32, 97.5 us (5.16 TB/s; a copy of 1 GiB reaches 5.20), from int8 codes 53 (3.8
+// fp32, 97 us (5.18 TB/s; a copy of 1 GiB reaches 5.20), from int8 codes 51 (3.9
 // TB/s; vector instructions: 8 an element); 24 ragged prompts of up to 384 tokens of
-// 12 heads of 64, int8, 16.5 us; 64 sequences of one token, fp32, 4.3 us, one 3.2 us.
+// 12 heads of 64, int8, 14.4 us; 64 sequences of one token, fp32, 4.3 us, one 3.1 us.
 //
 // cache_attention, few queries: each key and value byte is read once, for 4
 // operations and query head that shares it, so memory bounds it. Nothing passes
@@ -60,7 +60,10 @@ struct AppendArgs {
     const float *inv_freq;
     int64_t m;
     int32_t seq0, max_pages, n_pages, shift;  // 1 << shift: tokens of a page
-    int32_t nh, nkv, hd, cols, x_cb, q_cb;
+    int32_t nh, nkv, hd, x_cb, q_cb;
+    int32_t x_step, q_step;                   // bytes of a token's row, or of 16 tokens' blocks
+    uint32_t values;                          // bytes from a page's keys to its values
+    int64_t page_bytes;
     int32_t half, split;                      // rotated pairs of a head; 1: (j, j + half), 0: (2 j, 2 j + 1)
     int32_t q_columns, k_columns, v_columns;  // a thread each
     int32_t q_parts, k_parts, per, v_per;     // workgroups of queries and of keys, and columns of one
@@ -95,11 +98,22 @@ __device__ __forceinline__ void transpose_bytes(uint32_t (&w)[4])
     w[3] = __builtin_amdgcn_perm(d, b, 0x07060302u);
 }
 
-// A token's place in an activation, the same for a wave, and a feature's from there.
-__device__ __forceinline__ int64_t row_offset(int64_t t, int32_t cols, int32_t cb, int32_t size)
-{
-    return cb ? (t >> 4) * cb * 512 + (t & 15) * 32 : t * cols * size;
-}
+// The rows of some tokens, the same for a wave: the first one's, and where others begin from there. (64 bits for one of
+// them only: addresses of four rows took 200 scalar instructions a wave.)
+struct Rows {
+    int8_t *base;
+    int32_t step, phase;  // phase: the first one's place in its block of 16 tokens, or -1 for whole rows
+    __device__ __forceinline__ Rows(const int8_t *x, int32_t t, int32_t cb, int32_t bytes)
+        : base(const_cast<int8_t *>(x) + (int64_t)(cb ? t >> 4 : t) * bytes), step(bytes), phase(cb ? t & 15 : -1)
+    {
+    }
+    __device__ __forceinline__ int8_t *at(int32_t j) const
+    {
+        const int32_t i = phase + j;
+        return base + (phase < 0 ? j * step : (i >> 4) * step + (i & 15) * 32);
+    }
+};
+// A feature's place from its token's first.
 __device__ __forceinline__ uint32_t feature_offset(int32_t c, int32_t cb, int32_t size)
 {
     return cb ? (uint32_t)(c >> 5) * 512 + (c & 31) : (uint32_t)c * size;
@@ -236,13 +250,13 @@ __device__ __forceinline__ Tokens lengths(const AppendArgs &p, int32_t seq, int3
 }
 
 // The page that holds a slot, or NULL.
-__device__ __forceinline__ int8_t *page_of(const AppendArgs &p, int32_t seq, int64_t slot)
+__device__ __forceinline__ int8_t *page_of(const AppendArgs &p, int32_t seq, int32_t slot)
 {
-    const int64_t entry = slot >> p.shift;
+    const int32_t entry = slot >> p.shift;
     if (slot < 0 || entry >= p.max_pages) return nullptr;
     const int32_t number = ((ScalarTable)(uintptr_t)p.page_table)[(int64_t)seq * p.max_pages + entry];
     if ((uint32_t)number >= (uint32_t)p.n_pages) return nullptr;
-    return p.cache + (int64_t)number * (2 * p.nkv) * ((int64_t)p.hd << p.shift);
+    return p.cache + number * p.page_bytes;
 }
 
 // Which columns a workgroup has: `first` to `end` of the queries (0), keys (1) or values (2).
@@ -270,16 +284,16 @@ __global__ __launch_bounds__(256) void cache_append_step_kernel(const AppendArgs
     int32_t len;
     const Tokens tk = lengths(p, seq, len);
     for (int32_t i = 0; i < tk.n; ++i) {  // (one, unless a sequence has more than was said)
-        const int64_t t = (int64_t)tk.first + i, slot = (int64_t)len - tk.n + i;
-        const int8_t *row = p.x + row_offset(t, p.cols, p.x_cb, F32 ? 4 : 1);
-        const int32_t in_page = (int32_t)(slot & ((1 << p.shift) - 1));
+        const int32_t t = tk.first + i, slot = len - tk.n + i;
+        const int8_t *row = Rows(p.x, t, p.x_cb, p.x_step).at(0);
+        const int32_t in_page = slot & ((1 << p.shift) - 1);
         if (my.kind == 2) {
             const ValueColumn<F32> col(p, column);
             typename ValueColumn<F32>::Raw r{};
             if (mine) r = col.load(row);
             int8_t *page = page_of(p, seq, slot);
             if (!page || !mine) continue;
-            int8_t *to = page + ((int64_t)p.nkv << p.shift) * p.hd + (in_page & ~15) * p.hd + (in_page & 15);
+            int8_t *to = page + p.values + (in_page & ~15) * p.hd + (in_page & 15);
             const uint32_t w = col.codes(p, r);
 #pragma unroll
             for (int e = 0; e < 4; ++e) (to + 16 * e)[col.d0] = (int8_t)(w >> (8 * e));
@@ -297,7 +311,7 @@ __global__ __launch_bounds__(256) void cache_append_step_kernel(const AppendArgs
                 __syncthreads();
             }
             if (!mine || (my.kind && !page)) continue;
-            col.put(p, r0, r1, cs, sn, my.kind ? page + (int64_t)in_page * p.hd : p.q + row_offset(t, p.nh * p.hd, p.q_cb, 1),
+            col.put(p, r0, r1, cs, sn, my.kind ? page + in_page * p.hd : Rows(p.q, t, p.q_cb, p.q_step).at(0),
                     my.kind ? p.fk : p.fq);
         }
     }
@@ -315,18 +329,19 @@ __global__ __launch_bounds__(256) void cache_append_kernel(const AppendArgs p)
     const Share my = share_of(p, blockIdx.x);
     int32_t len;
     const Tokens tk = lengths(p, seq, len);
-    const int64_t p0 = (int64_t)len - tk.n;  // the first token's slot
-    for (int64_t s0 = (p0 & ~(int64_t)15) + (int64_t)blockIdx.y * 16; s0 < len && tk.n; s0 += (int64_t)gridDim.y * 16) {
+    const int32_t p0 = len - tk.n, ahead = p0 & 15;  // the first token's slot, and the slots before it in its 16
+    const int32_t groups = tk.n ? (tk.n + ahead + 15) >> 4 : 0;
+    for (int32_t g = blockIdx.y; g < groups; g += gridDim.y) {
         // slots from .. to - 1 of the 16 have a token, j0 .. j1 - 1 of the wave's 4
-        const int32_t from = (int32_t)(max(s0, p0) - s0), to = (int32_t)(min(s0 + 16, (int64_t)len) - s0);
+        const int32_t s0 = p0 - ahead + 16 * g, from = g ? 0 : ahead, to = min(tk.n + ahead - 16 * g, 16);
         const int32_t j0 = min(max(from - 4 * quad, 0), 4), j1 = min(max(to - 4 * quad, 0), 4);
-        const int64_t t0 = tk.first + (s0 - p0);  // slot j's token is t0 + j
-        const auto row = [&](int32_t j) { return p.x + row_offset(t0 + 4 * quad + j, p.cols, p.x_cb, F32 ? 4 : 1); };
-        const int32_t in_page = (int32_t)(s0 & ((1 << p.shift) - 1));
+        const int32_t t0 = tk.first - ahead + 16 * g + 4 * quad;  // the token of the wave's first slot
+        const Rows x(p.x, t0, p.x_cb, p.x_step);
+        const int32_t in_page = s0 & ((1 << p.shift) - 1);
         int8_t *page = my.kind ? page_of(p, seq, s0) : nullptr;
         if (my.kind == 2) {
             if (!page) continue;
-            int8_t *group = page + ((int64_t)p.nkv << p.shift) * p.hd + in_page * p.hd;
+            int8_t *group = page + p.values + in_page * p.hd;
             for (int32_t column = my.first; column < my.end; column += 64) {
                 const bool mine = column + lane < my.end;
                 const ValueColumn<F32> col(p, column + lane);
@@ -334,11 +349,11 @@ __global__ __launch_bounds__(256) void cache_append_kernel(const AppendArgs p)
                 if (j1 - j0 == 4) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        if (mine) r[j] = col.load(row(j));
+                        if (mine) r[j] = col.load(x.at(j));
                 } else {
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        if (mine && j >= j0 && j < j1) r[j] = col.load(row(j));
+                        if (mine && j >= j0 && j < j1) r[j] = col.load(x.at(j));
                 }
                 uint32_t w[4];
 #pragma unroll
@@ -375,15 +390,12 @@ __global__ __launch_bounds__(256) void cache_append_kernel(const AppendArgs p)
             for (int32_t i = lane; i < 4 * p.half; i += 64) {
                 const int32_t j = (int32_t)(((float)i + 0.5f) * p.inv_half), w = i - j * p.half;
                 if (j >= j0 && j < j1)
-                    angle(p, p.positions ? (double)p.positions[t0 + 4 * quad + j] : (double)(s0 + 4 * quad + j), w,
+                    angle(p, (double)(p.positions ? p.positions[t0 + j] : s0 + 4 * quad + j), w,
                           cs[4 * quad + j][w], sn[4 * quad + j][w]);
             }
             __syncthreads();
         }
-        const auto code_row = [&](int32_t j) {
-            return my.kind ? page + (int64_t)(in_page + 4 * quad + j) * p.hd
-                           : p.q + row_offset(t0 + 4 * quad + j, p.nh * p.hd, p.q_cb, 1);
-        };
+        const Rows y = my.kind ? Rows(page, in_page + 4 * quad, 0, p.hd) : Rows(p.q, t0, p.q_cb, p.q_step);
         const float f = my.kind ? p.fk : p.fq;
         for (int32_t column = my.first + lane; column < my.end; column += 64) {
             const PairColumn<F32, VEC> col(p, column, my.kind == 1);
@@ -391,22 +403,22 @@ __global__ __launch_bounds__(256) void cache_append_kernel(const AppendArgs p)
                 typename PairColumn<F32, VEC>::Raw r0[4], r1[4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    r0[j] = col.load(row(j), col.x0);
-                    r1[j] = col.load(row(j), col.x1);
+                    r0[j] = col.load(x.at(j), col.x0);
+                    r1[j] = col.load(x.at(j), col.x1);
                 }
 #pragma unroll
-                for (int j = 0; j < 4; ++j) col.put(p, r0[j], r1[j], cs[4 * quad + j], sn[4 * quad + j], code_row(j), f);
+                for (int j = 0; j < 4; ++j) col.put(p, r0[j], r1[j], cs[4 * quad + j], sn[4 * quad + j], y.at(j), f);
             } else {
                 typename PairColumn<F32, VEC>::Raw r0[4]{}, r1[4]{};
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     if (j < j0 || j >= j1) continue;
-                    r0[j] = col.load(row(j), col.x0);
-                    r1[j] = col.load(row(j), col.x1);
+                    r0[j] = col.load(x.at(j), col.x0);
+                    r1[j] = col.load(x.at(j), col.x1);
                 }
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    if (j >= j0 && j < j1) col.put(p, r0[j], r1[j], cs[4 * quad + j], sn[4 * quad + j], code_row(j), f);
+                    if (j >= j0 && j < j1) col.put(p, r0[j], r1[j], cs[4 * quad + j], sn[4 * quad + j], y.at(j), f);
             }
         }
     }
@@ -820,9 +832,13 @@ sl_status launch_cache_append(const sl_cache_append_args &a, void *stream)
     p.nh = a.n_heads;
     p.nkv = a.n_kv_heads;
     p.hd = a.head_dim;
-    p.cols = (a.n_heads + 2 * a.n_kv_heads) * a.head_dim;
-    p.x_cb = !f32 && a.x_layout == SL_LAYOUT_T16X32 ? (p.cols + 31) / 32 : 0;
+    const int32_t cols = (a.n_heads + 2 * a.n_kv_heads) * a.head_dim;
+    p.x_cb = !f32 && a.x_layout == SL_LAYOUT_T16X32 ? (cols + 31) / 32 : 0;
     p.q_cb = a.q_layout == SL_LAYOUT_T16X32 ? (a.n_heads * a.head_dim + 31) / 32 : 0;
+    p.x_step = p.x_cb ? p.x_cb * 512 : cols * (f32 ? 4 : 1);
+    p.q_step = p.q_cb ? p.q_cb * 512 : a.n_heads * a.head_dim;
+    p.values = (uint32_t)(a.n_kv_heads * a.head_dim) << p.shift;
+    p.page_bytes = 2 * (int64_t)p.values;
     p.half = a.rope_kind != SL_ROPE_NONE ? a.rope_dim / 2 : 0;
     p.split = a.rope_kind == SL_ROPE_HALF;
     p.rope_factor = a.rope_factor;
