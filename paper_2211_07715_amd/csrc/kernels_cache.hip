@@ -752,7 +752,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(const CacheArgs a)
 }
 
 struct Plan {
-    bool prompt;
+    bool prompt, by_length;
     int32_t tile_rows, splits, split_keys;
     int64_t tiles;
 };
@@ -764,19 +764,21 @@ Plan plan_of(const sl_cache_attention_args &a)
     const auto items_of = [&](int32_t tile_rows) {  // (a product of whole numbers may not fit)
         return (double)a.n_seq * a.n_kv_heads * (double)((rows + tile_rows - 1) / tile_rows);
     };
+    // (m_tokens bounds what sequences of different lengths have together: half a tile more each)
+    const auto real_of = [&](int32_t tile_rows) {
+        return std::min(items_of(tile_rows), (double)a.n_kv_heads * ((double)a.m_tokens * group / tile_rows + 0.5 * a.n_seq));
+    };
     // Tiles of 16 rows with the keys split as far as it takes, against 64 or 128 rows that share a chunk of keys (12 heads
     // of 64): 48 queries over 8192 keys (36 tiles of 16 rows) 15 us against 20, 8 times 48 over 2048 (288) 22 against 26,
     // 512 over 8192 (384) 42 against 42, 32 times 128 over 384 (eight times as many) 28 against 17; 8 heads of 128 that 4
     // share, 8 times 64 over 4096 (1024) 101 against 77.
-    Plan p{rows > 16 && items_of(16) > 384, 16, 1, 0, 0};
+    Plan p{rows > 16 && items_of(16) > 384, false, 16, 1, 0, 0};
     if (p.prompt) {
         // 64 rows, which two waves on either half of the chunks have, against 128 in four waves, where a workgroup has few
         // chunks or there are few (12 heads of 64): one of 2048 tokens (192 tiles of 128) 30 us against 36, 16 ragged ones
-        // (about 440) 46 against 61, 32 times 128 over 384 (384) 16.9 against 19.1; 4 times 2048 (768) 58 against 55, 32
-        // times 512 (1536) 46 against 38. (m_tokens bounds what sequences of different lengths have together: half a tile
-        // more each.) Wider heads have no room for two sets of chunks.
-        const double real = (double)a.n_kv_heads * ((double)a.m_tokens * group / 128 + 0.5 * a.n_seq);
-        p.tile_rows = a.head_dim <= 64 && (rows <= 64 || std::min(items_of(128), real) < 512) ? 64 : 128;
+        // (about 440) 36 against 49, 32 times 128 over 384 (384) 16.9 against 19.1; 4 times 2048 (768) 58 against 55, 32
+        // times 512 (1536) 46 against 38. Wider heads have no room for two sets of chunks.
+        p.tile_rows = a.head_dim <= 64 && (rows <= 64 || real_of(128) < 512) ? 64 : 128;
     }
     p.tiles = (rows + p.tile_rows - 1) / p.tile_rows;
     // Keys in parts, where there are too few tiles for the CUs and enough keys to pay for joining them (4 us and more): one
@@ -784,15 +786,25 @@ Plan plan_of(const sl_cache_attention_args &a)
     // 35, in one 40; 32 over 384 keys of 12 heads (384 tiles) in one 8.9, in 2 12.0. Of 128 rows: 8 times 64 over 4096 keys
     // of 8 heads of 128 that 4 share (128 tiles) in 3 77, in 6 85, in one 114; 64 times 16 over 1024 (512) in one 47, in
     // 2 69.
-    const double all = items_of(p.tile_rows);
+    const double all = p.prompt ? real_of(p.tile_rows) : items_of(16);
     const int32_t enough = p.prompt ? 384 : 512, least = p.prompt ? 1024 : 512;
-    if (all >= enough) return p;
-    const int64_t items = (int64_t)all;
-    const int64_t want = std::min<int64_t>((enough + items - 1) / items, ((int64_t)a.max_len + least - 1) / least);
+    int64_t want = 1;
+    if (all < enough) {
+        const int64_t items = std::max<int64_t>((int64_t)all, 1);
+        want = std::min<int64_t>((enough + items - 1) / items, ((int64_t)a.max_len + least - 1) / least);
+        // (tiles that sequences turn out not to have take workspace, and workgroups that join nothing)
+        want = (int64_t)std::min((double)want, 2048 / items_of(p.tile_rows));
+    }
     if (want > 1) {
         p.split_keys = (int32_t)((((int64_t)a.max_len + want - 1) / want + 255) / 256 * 256);
         p.splits = (int32_t)(((int64_t)a.max_len + p.split_keys - 1) / p.split_keys);
     }
+    // Prompts of different lengths: finding a tile's place takes each workgroup 1 to 1.5 us (32 times 128 over 384 keys 18.4
+    // against 16.8; one of 2000 tokens with two short ones 32.5 against 31.4), a good order of 16 ragged ones to 512 tokens
+    // behind to 2048 36 us against 47, of 64 121 against 137, of 4 in two parts 24.7 against 27.6. A lane is a sequence, and
+    // a workgroup for every CU needs no order.
+    p.by_length = p.prompt && a.n_seq > 1 && a.n_seq <= 64 && a.m_tokens < (int64_t)a.n_seq * a.max_new &&
+                  all * p.splits > 256;
     return p;
 }
 
@@ -940,6 +952,7 @@ sl_status launch_cache_attention(const sl_cache_attention_args &args, void *stre
     a.inv_group = 1.0f / a.group;
     a.group_shift = (a.group & (a.group - 1)) ? -1 : __builtin_ctz(a.group);
     a.tile_rows = p.tile_rows;
+    a.by_length = p.by_length;
     if (p.prompt) {
         const Exponent e = exponent_of((double)args.q_scale * args.k_scale * args.softmax_scale);
         a.c2 = e.c2;

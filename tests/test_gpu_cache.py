@@ -316,6 +316,26 @@ def test_attention_in_parts_of_more_than_said(hip, new):
     run_attend(hip, rng, b, 2)
 
 
+# prompts of different lengths, more than a workgroup for every CU: tiles in order of the keys that they see
+SORTED = [([100, 0, 7, 64, 65, 130, 1, 33], [100, 50, 300, 64, 1000, 140, 0, 33]), ([128, 128, 3, 128, 60], [128, 700, 3, 700, 2]),
+          ([300, 40], [300, 2300]), ([40] + [5, 0, 1] * 21, [41] + [70, 0, 9] * 21)]
+
+
+@pytest.mark.parametrize("news,lens", SORTED)
+@pytest.mark.parametrize("nh,nkv,hd", [(40, 40, 16), (24, 24, 64), (60, 20, 96), (24, 24, 128), (200, 2, 32)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_attention_in_order_of_length(hip, news, lens, nh, nkv, hd, causal):
+    rng = np.random.default_rng(20)
+    run_attend(hip, rng, Batch(hip, rng, news, lens, 16, nkv, hd, gap=1, holes=hd == 64), nh, causal=causal)
+
+
+def test_attention_in_order_of_more_than_said(hip):
+    rng = np.random.default_rng(21)
+    b = Batch(hip, rng, [3, 140] + [5] * 20, [30, 260] + [90] * 20, 16, 20, 64)
+    b.most_new, b.longest = 30, 100
+    run_attend(hip, rng, b, 20)
+
+
 def test_attention_long(hip):
     rng = np.random.default_rng(18)
     run_attend(hip, rng, Batch(hip, rng, [1, 2], [40000, 9999], 64, 1, 64), 8)
