@@ -774,11 +774,17 @@ Plan plan_of(const sl_cache_attention_args &a)
     // share, 8 times 64 over 4096 (1024) 101 against 77.
     Plan p{rows > 16 && items_of(16) > 384, false, 16, 1, 0, 0};
     if (p.prompt) {
-        // 64 rows, which two waves on either half of the chunks have, against 128 in four waves, where a workgroup has few
-        // chunks or there are few (12 heads of 64): one of 2048 tokens (192 tiles of 128) 30 us against 36, 16 ragged ones
-        // (about 440) 36 against 49, 32 times 128 over 384 (384) 16.9 against 19.1; 4 times 2048 (768) 58 against 55, 32
-        // times 512 (1536) 46 against 38. Wider heads have no room for two sets of chunks.
-        p.tile_rows = a.head_dim <= 64 && (rows <= 64 || real_of(128) < 512) ? 64 : 128;
+        // 64 rows, which two waves on either half of the chunks have, against 128 in four waves: half the chunks one after
+        // another, where those of the longest sequence are what a call waits for, for twice as many workgroups, of which
+        // 768 run at a time (12 heads of 64, tiles of 128; * 16 heads that share 4): 8 times 512 (384 tiles) 15 us against
+        // 18, 32 times 128 over 384 (384) 16.8 against 18.2, 16 ragged ones to 2560 keys (429) 36 against 49, 40 times 128
+        // over 384 (480) 21.4 against 19.0, 5 times 1024 (480) 26.4 against 28.8, one of 4096 (512*) 63 against 82, 4 times
+        // 1536 (576) 40.5 against 40.0, 2 times 3000 (574) 61 against 67, 4 times 1700 (662) 44 against 41, one of 6144
+        // (768*) 129 against 135, 4 times 2048 (768) 56 against 51, one of 8192 (1024*) 218 against 203; without causal,
+        // where all tiles are as long, 4 times 2000 of 8 heads of 32 (512) 57 against 52. Wider heads have no room for two
+        // sets of chunks.
+        const double real = real_of(128);
+        p.tile_rows = a.head_dim <= 64 && (rows <= 64 || (real <= 768 && a.max_len > (a.causal ? 12 : 24) * (real - 400))) ? 64 : 128;
     }
     p.tiles = (rows + p.tile_rows - 1) / p.tile_rows;
     // Keys in parts, where there are too few tiles for the CUs and enough keys to pay for joining them (4 us and more): one
