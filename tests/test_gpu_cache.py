@@ -8,9 +8,9 @@ Bars.
 - Attention: the weights' relative error is that of the exponential's argument x <= 24 that matters, |x| 2^-23 ln 2 (its
   factor's and its product's rounding), weighted with 2^-x under 1e-7 of the largest, over many keys of which each
   weighs little at most 24 * 2^-23 * ln 2 = 2e-6; the instruction's own 2^-22; and the whole number that stands for a
-  weight, 2^-24 of its span's largest, which the up to 128 keys of a span, all rounded one way, could add up to 2^-17 (the sum of
-  weights moves with it). Sums in 32 bits: 2^-24 for each of up to 100 additions, 6e-6. Together under 2e-5 of the
-  largest |v| = 127 v_scale, for the numerator and again for the denominator: TOL = 4e-5 * 127 v_scale.
+  weight, 2^-24 of its span's largest, which the up to 128 keys of a span, all rounded one way, could add up to 2^-17
+  (the sum of weights moves with it). Sums in 32 bits: 2^-24 for each of up to 100 additions, 6e-6. Together under 2e-5
+  of the largest |v| = 127 v_scale, for the numerator and again for the denominator: TOL = 4e-5 * 127 v_scale.
 """
 import numpy as np
 import pytest
@@ -329,11 +329,13 @@ def test_attention_in_order_of_length(hip, news, lens, nh, nkv, hd, causal):
     run_attend(hip, rng, Batch(hip, rng, news, lens, 16, nkv, hd, gap=1, holes=hd == 64), nh, causal=causal)
 
 
-def test_attention_in_order_of_more_than_said(hip):
+@pytest.mark.parametrize("longest", [100, 2100])  # (the second in two parts)
+def test_attention_in_order_of_more_than_said(hip, longest):
     rng = np.random.default_rng(21)
-    b = Batch(hip, rng, [3, 140] + [5] * 20, [30, 260] + [90] * 20, 16, 20, 64)
-    b.most_new, b.longest = 30, 100
+    b = Batch(hip, rng, [3, 140] + [5] * 20, [30, 2600] + [90] * 20, 16, 20, 64)
+    b.most_new, b.longest = 30, longest
     run_attend(hip, rng, b, 20)
+    assert hip.last_path() == f"cache prompt 64,{1 if longest == 100 else 2}"
 
 
 def test_attention_long(hip):
