@@ -618,19 +618,19 @@ def cache_append(x, cache, page_table, seq_start, kv_len, max_new: int, n_heads:
     torch = _torch or _torch_once()
     n_seq, pages, (n_pages, _, n_kv, page_size, head_dim), s = _cache_args(x, "x", cache, page_table, seq_start, kv_len,
                                                                            stream)
-    cols = (n_heads + 2 * n_kv) * head_dim
-    x_type = ACT_F32 if x.dtype is torch.float32 else ACT_I8
-    if x_type == ACT_I8 and x.dtype is not torch.int8:
+    cols, have, dt = (n_heads + 2 * n_kv) * head_dim, x.shape, x.dtype
+    x_type = ACT_F32 if dt is torch.float32 else ACT_I8
+    if x_type == ACT_I8 and dt is not torch.int8:
         raise ValueError("x must be float32 or int8")
     if x_layout == LAYOUT_T16X32:
         if x_type == ACT_F32 or m_tokens is None:
             raise ValueError("LAYOUT_T16X32 input is int8, and needs m_tokens")
-        if x.shape != t16x32_shape(m_tokens, cols):
+        if have != t16x32_shape(m_tokens, cols):
             raise ValueError(f"x must have shape {t16x32_shape(m_tokens, cols)}")
-    elif x.dim() != 2 or x.shape[1] != cols or (m_tokens is not None and m_tokens != x.shape[0]):
+    elif len(have) != 2 or have[1] != cols or (m_tokens is not None and m_tokens != have[0]):
         raise ValueError(f"x must be [{'M' if m_tokens is None else m_tokens}, {cols}]")
     else:
-        m_tokens = x.shape[0]
+        m_tokens = have[0]
     q = None
     if q_scale is not None:
         shape = t16x32_shape(m_tokens, n_heads * head_dim) if q_layout == LAYOUT_T16X32 else (m_tokens, n_heads * head_dim)
@@ -678,22 +678,22 @@ def cache_attention(q, cache, page_table, seq_start, kv_len, max_new: int, max_l
                                                                            stream)
     if q.dtype is not torch.int8:
         raise ValueError("q must be int8")
-    cols = n_heads * head_dim
+    cols, have = n_heads * head_dim, q.shape
     if q_layout == LAYOUT_T16X32:
         q_cols = cols if q_cols is None else q_cols
         if m_tokens is None:
             raise ValueError("m_tokens is required with LAYOUT_T16X32 input")
-        if q.shape != t16x32_shape(m_tokens, q_cols):
+        if have != t16x32_shape(m_tokens, q_cols):
             raise ValueError(f"q must have shape {t16x32_shape(m_tokens, q_cols)}")
-    elif q.dim() != 2 or (m_tokens is not None and m_tokens != q.shape[0]) or \
-            (q_cols is not None and q_cols != q.shape[1]) or q.shape[1] < cols:
+    elif len(have) != 2 or (m_tokens is not None and m_tokens != have[0]) or \
+            (q_cols is not None and q_cols != have[1]) or have[1] < cols:
         raise ValueError(f"q must be [{'M' if m_tokens is None else m_tokens}, {cols} or more]")
     else:
-        m_tokens, q_cols = q.shape
+        m_tokens, q_cols = have
     dt = _KIND_DTYPE.get(kind)
     shape = t16x32_shape(m_tokens, cols) if y_layout == LAYOUT_T16X32 else (m_tokens, cols)
     if out is None:  # (empty_like: 0.6 us less a call)
-        out = torch.empty_like(q) if dt is torch.int8 and q.shape == shape else torch.empty(shape, dtype=dt, device=q.device)
+        out = torch.empty_like(q) if dt is torch.int8 and have == shape else torch.empty(shape, dtype=dt, device=q.device)
     elif out.dtype is not dt or out.shape != shape or not out.is_contiguous() or out.device != q.device:
         raise ValueError("out has the wrong dtype/shape/device or is not contiguous")
     if softmax_scale is None:
