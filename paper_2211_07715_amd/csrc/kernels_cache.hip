@@ -32,10 +32,10 @@
 // rate; spans of 128 keys gave the same (99.6 us) and cost short sequences (5.4
 // against 4.7 us).
 //   Measured, replayed from a graph: 64 x 4096 tokens of 8 key heads of 128 with 4
-// query heads each 99 us (5.4 TB/s; reading alone reaches 6.4), 64 x 16384 376 (5.7),
+// query heads each 98.5 us (5.45 TB/s; reading alone reaches 6.4), 64 x 16384 374 (5.7),
 // 131072 tokens 57 to 61 (50 and 5 for the two launches), 24 ragged sequences of up
-// to 3001 tokens of 8 heads of 96 18.9 (2.7 TB/s: 17 and 4), 32 x 384 tokens of 12
-// heads of 64 8.7, 128 tokens 4.7. Vector instructions are active 30 % of the time
+// to 3001 tokens of 8 heads of 96 18.7 (2.75 TB/s: 16 and 4), 32 x 384 tokens of 12
+// heads of 64 8.4, 128 tokens 4.7. Vector instructions are active 30 % of the time
 // in the first, matrix ones 7 %.
 #include <hip/hip_runtime.h>
 #include <math.h>

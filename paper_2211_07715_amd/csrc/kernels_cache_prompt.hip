@@ -25,13 +25,13 @@
 // 204, and for heads of 128 (three waves against two) 170 to 184 against 187 in a
 // prompt of 4096 tokens of 32 heads, but 7 to 12 % more in shorter ones. Two tiles of
 // queries a wave 250 against 227 at the time. A prompt of a few chunks is the chain of
-// its loads and the first chunk's steps: of 16.5 us for 32 times 128 queries over 384
+// its loads and the first chunk's steps: of 16.7 us for 32 times 128 queries over 384
 // keys two thirds are not the chunks'.
 //
-// Measured, replayed from a graph, causal: 8192 tokens of 16 heads of 64 on 4 200 to
-// 212 us on different cards (650 to 690 TOP/s), 4096 of 32 heads of 128 on 8 187 (735),
+// Measured, replayed from a graph, causal: 8192 tokens of 16 heads of 64 on 4 193 to
+// 228 us on different cards (600 to 710 TOP/s), 4096 of 32 heads of 128 on 8 170 to 199,
 // 16 ragged prompts of up to 512 tokens behind up to 2048, 12 heads of 64, 36 (320),
-// 32 x 128 queries over 384 keys 16.5 (290). Two chunks between barriers took 203 to 210
+// 32 x 128 queries over 384 keys 16.7 (290). Two chunks between barriers took 203 to 210
 // us for 204, and sums of weights by 4x4 matrix instructions 220.
 #include <hip/hip_runtime.h>
 
