@@ -34,8 +34,9 @@
 //   Measured, replayed from a graph: 64 x 4096 tokens of 8 key heads of 128 with 4
 // query heads each 98.5 us (5.45 TB/s; reading alone reaches 6.4), 64 x 16384 374 (5.7),
 // 131072 tokens 57 to 61 (50 and 5 for the two launches), 24 ragged sequences of up
-// to 3001 tokens of 8 heads of 96 18.7 (2.75 TB/s: 16 and 4), 32 x 384 tokens of 12
-// heads of 64 8.4, 128 tokens 4.7. Vector instructions are active 30 % of the time
+// to 3001 tokens of 8 heads of 96 18.7 (2.75 TB/s: 16 and 4), 64 ragged ones of
+// up to 4096 of 8 heads of 128 55 (4.6), 32 x 384 tokens of 12 heads of 64 8.4, 128
+// tokens 4.7. Vector instructions are active 30 % of the time
 // in the first, matrix ones 7 %.
 #include <hip/hip_runtime.h>
 #include <math.h>
@@ -464,7 +465,8 @@ __device__ __forceinline__ void store_row(const CacheArgs &a, int64_t tok, int32
             codes_of(v, g * a.inv_so);
 }
 
-template <int F>
+// SORTED: where sequences turn out to differ in length, those that see the most keys come first.
+template <int F, bool SORTED>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(3))) void cache_split_kernel(const CacheArgs a)
 {
     constexpr int N = (F + 3) / 4, HD = 16 * F, FB = 2;
@@ -472,20 +474,59 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(3))
     __shared__ int32_t ms[kWaves][16];
     __shared__ float ls[kWaves][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, h = lane >> 4;
-    const int32_t split = blockIdx.z, seq = a.seq0 + blockIdx.y;
-    const int32_t kv = a.tiles == 1 ? blockIdx.x : blockIdx.x / (uint32_t)a.tiles, tile0 = blockIdx.x - kv * a.tiles;
-    const int32_t *table = a.page_table + (int64_t)seq * a.max_pages;
+    int32_t split = blockIdx.z, seq = a.seq0 + blockIdx.y;
+    int32_t kv = a.tiles == 1 ? blockIdx.x : blockIdx.x / (uint32_t)a.tiles, tile0 = blockIdx.x - kv * a.tiles;
     const int32_t last_entry = a.max_pages - 1, in_mask = (1 << a.shift) - 1;
     // pages of the 16 keys that the lane's row of the scores' left operand and its values come from
     int32_t pk = -1, pv = -1;
     const auto entries = [&](int32_t kb) __attribute__((always_inline)) {
+        const int32_t *table = a.page_table + (int64_t)seq * a.max_pages;
         pk = table[min((kb + 16 * (r >> 2)) >> a.shift, last_entry)];
         pv = table[min((kb + 16 * h) >> a.shift, last_entry)];
     };
     if (a.max_pages) entries(split * a.split_keys + wave * kSpan);  // (on their way with the lengths)
-    int32_t b0 = ((ScalarTable)(uintptr_t)a.seq_start)[seq], b1 = ((ScalarTable)(uintptr_t)a.seq_start)[seq + 1];
-    int32_t len = ((ScalarTable)(uintptr_t)a.kv_len)[seq];
-    asm volatile("" : "+s"(b0), "+s"(b1), "+s"(len));  // (here they are all waited for, instead of one after the other)
+    int32_t b0, b1, len;
+    if constexpr (!SORTED) {
+        b0 = ((ScalarTable)(uintptr_t)a.seq_start)[seq];
+        b1 = ((ScalarTable)(uintptr_t)a.seq_start)[seq + 1];
+        len = ((ScalarTable)(uintptr_t)a.kv_len)[seq];
+        asm volatile("" : "+s"(b0), "+s"(b1), "+s"(len));  // (here they are all waited for, instead of one after the other)
+    } else {
+        const auto place = [&](const auto &all, auto sets) __attribute__((always_inline)) {
+            if (all.equal(a, lane)) {
+#pragma unroll
+                for (int g = 0; g < sets; ++g) {
+                    if (seq / 64 != g) continue;
+                    b0 = __builtin_amdgcn_readlane(all.start[g], seq % 64);
+                    b1 = __builtin_amdgcn_readlane(all.end[g], seq % 64);
+                    len = __builtin_amdgcn_readlane(all.len[g], seq % 64);
+                }
+                return true;
+            }
+            // (every second 256 workgroups backwards, as prompts have them)
+            uint32_t number = blockIdx.x + gridDim.x * (blockIdx.y + gridDim.y * blockIdx.z);
+            const uint32_t of = number % 256;
+            if ((number / 256 & 1) && number - of + 256 <= gridDim.x * gridDim.y * gridDim.z)
+                number = number - of + 248 - (of & ~7u) + of % 8;
+            const uint32_t rest = number / (uint32_t)a.n_kv, most = gridDim.y * a.tiles;
+            kv = number - rest * a.n_kv;
+            split = a.splits == 1 ? 0 : rest / most;
+            const Place at = nth_longest(a, all, rest - split * most, 16);
+            if (at.seq < 0) return false;
+            seq = at.seq;
+            b0 = at.start;
+            b1 = at.end;
+            len = at.len;
+            tile0 = (int32_t)((((int64_t)tokens_between(b0, b1, a.m).n * a.group + 15) / 16 - 1 - at.from_last) % a.tiles);
+            if (a.max_pages) entries(split * a.split_keys + wave * kSpan);
+            return true;
+        };
+        if (a.n_seq <= 64) {
+            if (!place(Lengths<1>(a, lane), std::integral_constant<int, 1>{})) return;
+        } else {
+            if (!place(Lengths<kMostSorted / 64>(a, lane), std::integral_constant<int, kMostSorted / 64>{})) return;
+        }
+    }
     const Tokens tk = tokens_between(b0, b1, a.m);
     const int64_t rows = (int64_t)tk.n * a.group;
     len = max(len, 0);
@@ -807,17 +848,24 @@ Plan plan_of(const sl_cache_attention_args &a)
     }
     // Prompts of different lengths: finding a tile's place takes each workgroup 1 to 1.5 us (32 times 128 over 384 keys 18.4
     // against 16.8; one of 2000 tokens with two short ones 32.5 against 31.4), a good order of 16 ragged ones to 512 tokens
-    // behind to 2048 36 us against 47, of 64 121 against 137, of 4 in two parts 24.7 against 27.6. A lane is a sequence, and
-    // a workgroup for every CU needs no order.
-    p.by_length = p.prompt && a.n_seq > 1 && a.n_seq <= 64 && a.m_tokens < (int64_t)a.n_seq * a.max_new &&
-                  all * p.splits > 256;
+    // behind to 2048 35.5 us against 47, of 64 121 against 137, of 4 in two parts 24.7 against 27.6. A workgroup for every
+    // CU needs no order.
+    //   Steps, whose lengths only the device knows: sequences of one length go on at once (64 times 4096 of 8 heads of 128
+    // 99.5 us against 99.1), ragged ones to 4096 take 55 against 65, 128 of them 119 against 127, 32 to 8192 56 against 72;
+    // 40 to 3000 of 12 heads of 64, which could be 184 MB, 29.7 against 28.5.
+    const bool differ = p.prompt ? a.m_tokens < (int64_t)a.n_seq * a.max_new && all * p.splits > 256
+                                 : (double)a.n_seq * a.n_kv_heads * a.max_len * 2 * a.head_dim >= 0x1p28;
+    p.by_length = differ && a.n_seq > 1 && a.n_seq <= kMostSorted;
     return p;
 }
 
 template <int F>
 sl_status launch_split(const CacheArgs &a, dim3 grid, hipStream_t s)
 {
-    hipLaunchKernelGGL((cache_split_kernel<F>), grid, dim3(64 * kWaves), 0, s, a);
+    if (a.by_length)
+        hipLaunchKernelGGL((cache_split_kernel<F, true>), grid, dim3(64 * kWaves), 0, s, a);
+    else
+        hipLaunchKernelGGL((cache_split_kernel<F, false>), grid, dim3(64 * kWaves), 0, s, a);
     HIP_TRY(hipGetLastError());
     return SL_OK;
 }

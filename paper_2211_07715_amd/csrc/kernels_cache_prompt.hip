@@ -41,67 +41,6 @@ namespace sl {
 
 namespace {
 
-// v of a lane and those before it: their sum, or the largest.
-template <class F>
-__device__ __forceinline__ int32_t running(int32_t v, int32_t none, F with)
-{
-    v = with(v, __builtin_amdgcn_update_dpp(none, v, 0x111, 0xf, 0xf, false));  // 1, 2, 4, 8 lanes before in 16
-    v = with(v, __builtin_amdgcn_update_dpp(none, v, 0x112, 0xf, 0xf, false));
-    v = with(v, __builtin_amdgcn_update_dpp(none, v, 0x114, 0xf, 0xf, false));
-    v = with(v, __builtin_amdgcn_update_dpp(none, v, 0x118, 0xf, 0xf, false));
-    v = with(v, __builtin_amdgcn_update_dpp(none, v, 0x142, 0xa, 0xf, false));  // lanes 15 and 47 to the 16 after them
-    return with(v, __builtin_amdgcn_update_dpp(none, v, 0x143, 0xc, 0xf, false));  // lane 31 to the last 32
-}
-__device__ __forceinline__ int32_t running_sum(int32_t v)
-{
-    return running(v, 0, [](int32_t x, int32_t y) { return x + y; });
-}
-__device__ __forceinline__ int32_t lanes_sum(int32_t v) { return __builtin_amdgcn_readlane(running_sum(v), 63); }
-__device__ __forceinline__ int32_t lanes_max(int32_t v)  // (of numbers that are not below 0)
-{
-    return __builtin_amdgcn_readlane(running(v, 0, [](int32_t x, int32_t y) { return max(x, y); }), 63);
-}
-
-struct Place {
-    int32_t seq, from_last, start, end, len;  // a tile's sequence (-1: none), its number from the last, the lengths
-};
-// Tile `nth` of all sequences', those that see the most keys first. A lane is a sequence. Its last tile's level says by
-// how many tiles' tokens it is shorter than the longest, tile j before that is on the jth level after it (without
-// `causal` on the same). How many tiles lie above a level is a sum over lanes, so tile nth's level is found by halves.
-__device__ __forceinline__ Place nth_longest(const CacheArgs &a, int32_t nth, int32_t lane, int32_t tile_rows)
-{
-    int32_t start = 0, end = 0, len = 0;
-    if (lane < a.n_seq) {
-        start = a.seq_start[lane];
-        end = a.seq_start[lane + 1];
-        len = a.kv_len[lane];
-    }
-    const int64_t rows = (int64_t)tokens_between(start, end, a.m).n * a.group;
-    const int32_t tiles = (int32_t)min((rows + tile_rows - 1) / tile_rows, (int64_t)a.tiles);
-    const int32_t keys = (int32_t)min((int64_t)max(len, 0), (int64_t)a.max_pages << a.shift);
-    const int32_t level = (int32_t)((uint32_t)(lanes_max(keys) - keys) / (uint32_t)max(tile_rows / a.group, 1));
-    const auto above = [&](int32_t l) { return a.causal ? min(max(l - level, 0), tiles) : l > level ? tiles : 0; };
-    int32_t lo = 0, hi = lanes_max(level + tiles);
-    Place at{-1, 0, 0, 0, 0};
-    if (nth >= lanes_sum(tiles)) return at;
-    while (hi - lo > 1) {
-        const int32_t mid = lo + (hi - lo) / 2;
-        if (lanes_sum(above(mid)) <= nth)
-            lo = mid;
-        else
-            hi = mid;
-    }
-    const int32_t mine = above(lo + 1) - above(lo), before = running_sum(mine) - mine, rest = nth - lanes_sum(above(lo));
-    const uint64_t found = __ballot(before <= rest && rest < before + mine);
-    at.seq = __builtin_ctzll(found);
-    const int32_t its_level = __builtin_amdgcn_readlane(level, at.seq), its_first = __builtin_amdgcn_readlane(before, at.seq);
-    at.from_last = a.causal ? lo - its_level : rest - its_first;
-    at.start = __builtin_amdgcn_readlane(start, at.seq);
-    at.end = __builtin_amdgcn_readlane(end, at.seq);
-    at.len = __builtin_amdgcn_readlane(len, at.seq);
-    return at;
-}
-
 // N: 32-feature tiles of a head. A wave has 32 queries; RW waves share a chunk of
 // keys, and the 4 / RW sets of them in a workgroup have the same queries and take
 // turns at the chunks, until their m, l and O meet in LDS at the end.
@@ -124,7 +63,7 @@ void cache_prompt_kernel(const CacheArgs a)
     // differ in length and are few, in that very order (nth_longest). With several sequences every second 256 workgroups
     // go backwards (in eights, so that an XCD keeps its heads): their CUs have work of the 256 before them, and what is
     // long there meets what is short. (16 sequences of up to 512 tokens behind up to 2048, 12 heads: 55 us in the order of
-    // sequences, 47 with every second 256 backwards, 36 sorted; one of 8192, in order of length as it is: 213 backwards,
+    // sequences, 47 with every second 256 backwards, 35.5 sorted; one of 8192, in order of length as it is: 213 backwards,
     // 204 not.)
     uint32_t head = blockIdx.x, nth = blockIdx.y, turn = blockIdx.z;
     if (gridDim.y > 1) {
@@ -140,7 +79,8 @@ void cache_prompt_kernel(const CacheArgs a)
     if (a.by_length) {
         const uint32_t rest = nth + gridDim.y * turn;
         const int32_t tile = a.splits == 1 ? rest : rest / (uint32_t)a.splits;
-        const Place at = nth_longest(a, tile, lane, TQ);
+        const Place at = a.n_seq <= 64 ? nth_longest(a, Lengths<1>(a, lane), tile, TQ)
+                                       : nth_longest(a, Lengths<kMostSorted / 64>(a, lane), tile, TQ);
         if (at.seq < 0) return;
         seq = at.seq;
         from_last = at.from_last;

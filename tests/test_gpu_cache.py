@@ -338,6 +338,29 @@ def test_attention_in_order_of_more_than_said(hip, longest):
     assert hip.last_path() == f"cache prompt 64,{1 if longest == 100 else 2}"
 
 
+@pytest.mark.parametrize("n,nh,nkv,hd", [(3, 4, 2, 64), (64, 8, 8, 16), (70, 16, 8, 128), (256, 3, 1, 96), (257, 2, 2, 32)])
+@pytest.mark.parametrize("equal", [False, True])
+@pytest.mark.parametrize("causal", [True, False])
+def test_attention_of_steps_that_may_be_long(hip, n, nh, nkv, hd, equal, causal):
+    """Steps sized for 2^28 bytes of cache and more, where the sequences with the most keys come first."""
+    rng = np.random.default_rng(n + hd)
+    lens = [130] * n if equal else [int(k) for k in rng.integers(0, 300, n)]
+    news = [1] * n if equal else [int(k) for k in rng.integers(0, 4, n)]
+    b = Batch(hip, rng, news, lens, 16, nkv, hd, gap=2, holes=hd == 16)
+    b.longest = 2 ** 28 // (n * nkv * 2 * hd) + 1
+    run_attend(hip, rng, b, nh, causal=causal)
+    b.most_new = 1  # (where some have more)
+    run_attend(hip, rng, b, nh, causal=causal)
+
+
+def test_attention_of_long_steps_in_parts(hip):
+    rng = np.random.default_rng(22)
+    b = Batch(hip, rng, [1, 3, 1, 0, 1, 1], [5000, 40, 9000, 700, 0, 2600], 64, 2, 128)
+    b.longest = 90000
+    run_attend(hip, rng, b, 8)
+    assert hip.last_path() == "cache split 128,40"  # of 90000 / 43 keys, up to the next 256: 2304
+
+
 def test_attention_long(hip):
     rng = np.random.default_rng(18)
     run_attend(hip, rng, Batch(hip, rng, [1, 2], [40000, 9999], 64, 1, 64), 8)
