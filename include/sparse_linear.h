@@ -465,8 +465,8 @@ sl_status cache_append(const sl_cache_append_args *args, void *hip_stream);
  * Other fields as in cache_append. Softmax weights enter the products with 23 bits
  * of the largest of 64 keys, or, for many queries, as in attention_run. Results do
  * not depend on timing.
- * Errors: SL_ERR_INVALID_ARG, SL_ERR_SHAPE (sizes), SL_ERR_UNSUPPORTED (more
- * work items than a launch takes).
+ * Errors: SL_ERR_INVALID_ARG, SL_ERR_SHAPE (sizes), SL_ERR_UNSUPPORTED (n_seq *
+ * n_kv_heads from 2^23 on: more workgroups than a launch takes).
  */
 typedef struct {
     const int8_t *q;

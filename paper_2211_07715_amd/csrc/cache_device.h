@@ -2,6 +2,7 @@
 #pragma once
 
 #include "attention_device.h"
+#include "cache_plan.h"
 
 namespace sl {
 
@@ -70,7 +71,6 @@ __device__ __forceinline__ int32_t lanes_max(int32_t v)  // (of numbers that are
 }
 
 // The lengths of all sequences of a call that has few, up to S of them a lane.
-constexpr int kMostSorted = 256;
 template <int S>
 struct Lengths {
     int32_t start[S], end[S], len[S];

@@ -46,6 +46,7 @@
 #include <type_traits>
 
 #include "cache_device.h"
+#include "cache_plan.h"
 #include "encoder.h"
 
 namespace sl {
@@ -792,73 +793,6 @@ __global__ __launch_bounds__(256) void cache_join_kernel(const CacheArgs a)
     }
 }
 
-struct Plan {
-    bool prompt, by_length;
-    int32_t tile_rows, splits, split_keys;
-    int64_t tiles;
-};
-
-Plan plan_of(const sl_cache_attention_args &a)
-{
-    const int32_t group = a.n_heads / a.n_kv_heads;
-    const int64_t rows = (int64_t)a.max_new * group;
-    const auto items_of = [&](int32_t tile_rows) {  // (a product of whole numbers may not fit)
-        return (double)a.n_seq * a.n_kv_heads * (double)((rows + tile_rows - 1) / tile_rows);
-    };
-    // (m_tokens bounds what sequences of different lengths have together: half a tile more each)
-    const auto real_of = [&](int32_t tile_rows) {
-        return std::min(items_of(tile_rows), (double)a.n_kv_heads * ((double)a.m_tokens * group / tile_rows + 0.5 * a.n_seq));
-    };
-    // Tiles of 16 rows with the keys split as far as it takes, against 64 or 128 rows that share a chunk of keys (12 heads
-    // of 64): 48 queries over 8192 keys (36 tiles of 16 rows) 15 us against 20, 8 times 48 over 2048 (288) 22 against 26,
-    // 512 over 8192 (384) 42 against 42, 32 times 128 over 384 (eight times as many) 28 against 17; 8 heads of 128 that 4
-    // share, 8 times 64 over 4096 (1024) 101 against 77.
-    Plan p{rows > 16 && items_of(16) > 384, false, 16, 1, 0, 0};
-    if (p.prompt) {
-        // 64 rows, which two waves on either half of the chunks have, against 128 in four waves: half the chunks one after
-        // another, where those of the longest sequence are what a call waits for, for twice as many workgroups, of which
-        // 768 run at a time (12 heads of 64, tiles of 128; * 16 heads that share 4): 8 times 512 (384 tiles) 15 us against
-        // 18, 32 times 128 over 384 (384) 16.8 against 18.2, 16 ragged ones to 2560 keys (429) 36 against 49, 40 times 128
-        // over 384 (480) 21.4 against 19.0, 5 times 1024 (480) 26.4 against 28.8, one of 4096 (512*) 63 against 82, 4 times
-        // 1536 (576) 40.5 against 40.0, 2 times 3000 (574) 61 against 67, 4 times 1700 (662) 44 against 41, one of 6144
-        // (768*) 129 against 135, 4 times 2048 (768) 56 against 51, one of 8192 (1024*) 218 against 203; without causal,
-        // where all tiles are as long, 4 times 2000 of 8 heads of 32 (512) 57 against 52. Wider heads have no room for two
-        // sets of chunks.
-        const double real = real_of(128);
-        p.tile_rows = a.head_dim <= 64 && (rows <= 64 || (real <= 768 && a.max_len > (a.causal ? 12 : 24) * (real - 400))) ? 64 : 128;
-    }
-    p.tiles = (rows + p.tile_rows - 1) / p.tile_rows;
-    // Keys in parts, where there are too few tiles for the CUs and enough keys to pay for joining them (4 us and more): one
-    // query over 131072 keys of 8 heads of 128 in 64 parts 58 us, in 32 58, in 128 61, in one 873; 16 queries over 4096 in 4
-    // 35, in one 40; 32 over 384 keys of 12 heads (384 tiles) in one 8.9, in 2 12.0. Of 128 rows: 8 times 64 over 4096 keys
-    // of 8 heads of 128 that 4 share (128 tiles) in 3 77, in 6 85, in one 114; 64 times 16 over 1024 (512) in one 47, in
-    // 2 69.
-    const double all = p.prompt ? real_of(p.tile_rows) : items_of(16);
-    const int32_t enough = p.prompt ? 384 : 512, least = p.prompt ? 1024 : 512;
-    int64_t want = 1;
-    if (all < enough) {
-        const int64_t items = std::max<int64_t>((int64_t)all, 1);
-        want = std::min<int64_t>((enough + items - 1) / items, ((int64_t)a.max_len + least - 1) / least);
-        // (tiles that sequences turn out not to have take workspace, and workgroups that join nothing)
-        want = (int64_t)std::min((double)want, 2048 / items_of(p.tile_rows));
-    }
-    if (want > 1) {
-        p.split_keys = (int32_t)((((int64_t)a.max_len + want - 1) / want + 255) / 256 * 256);
-        p.splits = (int32_t)(((int64_t)a.max_len + p.split_keys - 1) / p.split_keys);
-    }
-    // Prompts of different lengths: finding a tile's place takes each workgroup 1 to 1.5 us (32 times 128 over 384 keys 18.4
-    // against 16.8; one of 2000 tokens with two short ones 32.5 against 31.4), a good order of 16 ragged ones to 512 tokens
-    // behind to 2048 35.5 us against 47, of 64 121 against 137, of 4 in two parts 24.7 against 27.6. A workgroup for every
-    // CU needs no order.
-    //   Steps, whose lengths only the device knows: sequences of one length go on at once (64 times 4096 of 8 heads of 128
-    // 99.5 us against 99.1), ragged ones to 4096 take 55 against 65, 128 of them 119 against 127, 32 to 8192 56 against 72;
-    // 40 to 3000 of 12 heads of 64, which could be 184 MB, 29.7 against 28.5.
-    const bool differ = p.prompt ? a.m_tokens < (int64_t)a.n_seq * a.max_new && all * p.splits > 256
-                                 : (double)a.n_seq * a.n_kv_heads * a.max_len * 2 * a.head_dim >= 0x1p28;
-    p.by_length = differ && a.n_seq > 1 && a.n_seq <= kMostSorted;
-    return p;
-}
-
 template <int F>
 sl_status launch_split(const CacheArgs &a, dim3 grid, hipStream_t s)
 {
@@ -874,7 +808,7 @@ sl_status launch_split(const CacheArgs &a, dim3 grid, hipStream_t s)
 
 int64_t cache_attention_bytes(const sl_cache_attention_args &a)
 {
-    const Plan p = plan_of(a);
+    const AttentionPlan p = plan_of(a);
     if (p.splits == 1) return 0;
     return (int64_t)a.n_seq * a.n_kv_heads * p.tiles * p.splits * record(a.head_dim, p.tile_rows) * 4;
 }
@@ -920,7 +854,6 @@ sl_status launch_cache_append(const sl_cache_append_args &a, void *stream)
     p.inv_value = 4.0f / a.head_dim;
     p.inv_half = p.half ? 1.0f / p.half : 0.0f;
     const bool step = a.max_new == 1;
-    constexpr int32_t kMostGrid = 65535;  // workgroups of a launch in its second and third dimension
     // (the first may begin anywhere in 16 slots; a launch of fewer goes through them in turns)
     const int64_t groups = step ? 1 : std::min<int64_t>(((int64_t)a.max_new + 30) / 16, kMostGrid);
     // Columns of a workgroup: in a step one a thread; else as many as leave 4096 workgroups, since each of them computes
@@ -978,14 +911,13 @@ sl_status launch_cache_attention(const sl_cache_attention_args &args, void *stre
     a.y = args.y;
     a.work = static_cast<float *>(args.workspace);
     a.m = args.m_tokens;
-    const Plan p = plan_of(args);
-    constexpr int32_t kMostGrid = 65535;  // workgroups of a launch in its second and third dimension
-    if ((double)args.n_seq * args.n_kv_heads * (double)p.tiles * p.splits > 0x7fffffff / 256) {
+    const AttentionPlan p = plan_of(args);
+    if (!p.fits) {
         set_error("too many work items for one launch");
         return SL_ERR_UNSUPPORTED;
     }
     a.n_seq = args.n_seq;
-    a.tiles = (int32_t)(p.prompt ? std::min<int64_t>(p.tiles, kMostGrid / p.splits) : p.tiles);
+    a.tiles = p.tiles;
     a.splits = p.splits;
     a.split_keys = p.split_keys;
     a.n_heads = args.n_heads;

@@ -1,0 +1,35 @@
+"""What calls of a decoder's cache launch, on the CPU: batches of prompts and steps together are within a launch's limits
+however long the prompts are, and the calls of the GPU tests take the paths that they are there for."""
+import pytest
+
+import cache_plan as plan
+from test_gpu_cache_mixed import MIXED
+
+ITEMS, GRID = 2 ** 23 - 1, 65535
+
+
+@pytest.mark.parametrize("n_seq,prompt,nh,nkv,hd", [
+    (256, 131072, 32, 8, 128), (2049, 32768, 32, 8, 128), (2, 2 ** 30, 32, 8, 128), (65536, 65536, 12, 12, 64), (1, 2 ** 31 - 256, 16, 4, 64), (4096, 8192, 64, 1, 64)])
+def test_one_prompt_beside_steps(n_seq, prompt, nh, nkv, hd):
+    for causal in (True, False):
+        p = plan.attention(n_seq - 1 + prompt, n_seq, prompt, prompt, nh, nkv, hd, causal)
+        assert p.fits and p.prompt and p.tiles > 0
+        assert n_seq * nkv * p.tiles * p.splits <= ITEMS and p.tiles * p.splits <= GRID
+        assert p.tiles * p.tile_rows <= prompt * (nh // nkv) + p.tile_rows - 1
+
+
+@pytest.mark.parametrize("n,at,prompt,nh,nkv,hd", MIXED)
+def test_mixed_batches_have_more_tiles_than_workgroups(n, at, prompt, nh, nkv, hd):
+    p = plan.attention(n - 1 + prompt, n, prompt, prompt, nh, nkv, hd)
+    tiles = -(-prompt * (nh // nkv) // p.tile_rows)
+    assert p.prompt and p.by_length == (n <= 256) and p.splits == 1 and 1 < p.tiles < tiles and n * nkv * tiles > ITEMS
+
+
+def test_what_fits_has_a_workgroup_for_every_tile():
+    p = plan.attention(16 * 300, 16, 512, 2560, 12, 12, 64)
+    assert p.fits and p.tiles == 512 // p.tile_rows
+
+
+def test_one_tile_a_sequence_does_not_fit():
+    assert plan.attention(2 ** 20, 2 ** 20, 1, 64, 8, 8, 64).fits == 0  # 2^23 tiles
+    assert plan.attention(2 ** 20, 2 ** 20 - 1, 1, 64, 8, 8, 64).fits == 1
