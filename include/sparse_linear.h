@@ -403,8 +403,8 @@ typedef enum {
  *   rope_dim    even, 2 .. head_dim; inv_freq slower and rope_factor other than 1
  *               serve contexts scaled beyond the trained ones
  * cache and q overlap no input. Allocates nothing, never synchronises.
- * Errors: SL_ERR_INVALID_ARG, SL_ERR_SHAPE (sizes), SL_ERR_UNSUPPORTED (more
- * work items than a launch takes).
+ * Errors: SL_ERR_INVALID_ARG, SL_ERR_SHAPE (sizes), SL_ERR_UNSUPPORTED (n_seq
+ * times the workgroups that a token's features take, 2 or more, from 2^23 on).
  */
 typedef struct {
     const void *x;

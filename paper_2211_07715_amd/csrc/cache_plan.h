@@ -84,4 +84,46 @@ inline AttentionPlan plan_of(const sl_cache_attention_args &a)
     return p;
 }
 
+struct AppendPlan {
+    bool fits, step, vec;                     // (vec: 8 features a thread of queries and keys, else 2)
+    int32_t groups;                           // workgroups for a sequence's groups of 16 slots
+    int32_t q_columns, k_columns, v_columns;  // a thread each
+    int32_t q_parts, k_parts, parts;          // workgroups of queries, of keys, and of all columns
+    int32_t per, v_per;                       // columns of one
+};
+
+inline AppendPlan plan_of(const sl_cache_append_args &a)
+{
+    AppendPlan p{};
+    p.vec = a.rope_kind == SL_ROPE_NONE || a.rope_dim % 8 == 0;
+    const int32_t width = p.vec ? 8 : 2;
+    p.q_columns = a.q ? a.n_heads * (a.head_dim / width) : 0;
+    p.k_columns = a.n_kv_heads * (a.head_dim / width);
+    p.v_columns = a.n_kv_heads * (a.head_dim / 4);
+    p.step = a.max_new == 1;
+    // (the first may begin anywhere in 16 slots; a launch of fewer goes through them in turns)
+    const int64_t groups = p.step ? 1 : std::min<int64_t>(((int64_t)a.max_new + 30) / 16, kMostGrid);
+    // Columns of a workgroup: in a step one a thread; else as many as leave 4096 workgroups, since each of them computes
+    // its tokens' angles (4 x 4096 tokens of 32 heads of 128 that 4 share: 99.5 us from fp32 and 54 from int8; with 1024
+    // 105.8 and 52, with 16384 98 and 73; ragged prompts, which have fewer in all, 17.7 to 17.8).
+    const auto even = [](int32_t columns, int32_t most) {  // in equal parts of at most so many
+        const int32_t parts = std::max((columns + most - 1) / most, 1);
+        return std::max((columns + parts - 1) / parts, 1);
+    };
+    const double tokens = std::min((double)groups * a.n_seq, (double)a.m_tokens / 16 + a.n_seq);
+    int32_t most = 256;
+    if (!p.step)
+        while (most > 64 && tokens * (p.q_columns + p.k_columns + p.v_columns) / most < 4096) most /= 2;
+    p.per = even(std::max(p.q_columns, p.k_columns), most);
+    p.v_per = even(p.v_columns, most);
+    p.q_parts = (p.q_columns + p.per - 1) / p.per;
+    p.k_parts = (p.k_columns + p.per - 1) / p.per;
+    p.parts = p.q_parts + p.k_parts + (p.v_columns + p.v_per - 1) / p.v_per;
+    // (as cache_attention's tiles: what has no workgroup of its own is done in turns)
+    const int64_t room = kMostItems / ((int64_t)a.n_seq * p.parts);
+    p.fits = room > 0;
+    p.groups = (int32_t)std::min(groups, room);
+    return p;
+}
+
 }  // namespace sl

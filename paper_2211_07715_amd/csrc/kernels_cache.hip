@@ -815,7 +815,12 @@ int64_t cache_attention_bytes(const sl_cache_attention_args &a)
 
 sl_status launch_cache_append(const sl_cache_append_args &a, void *stream)
 {
-    const bool f32 = a.x_type == SL_ACT_F32, vec = a.rope_kind == SL_ROPE_NONE || a.rope_dim % 8 == 0;
+    const AppendPlan plan = plan_of(a);
+    if (!plan.fits) {
+        set_error("too many work items for one launch");
+        return SL_ERR_UNSUPPORTED;
+    }
+    const bool f32 = a.x_type == SL_ACT_F32;
     AppendArgs p{};
     p.x = static_cast<const int8_t *>(a.x);
     p.q = a.q;
@@ -846,52 +851,33 @@ sl_status launch_cache_append(const sl_cache_append_args &a, void *stream)
     p.fq = factor(a.q_scale);
     p.fk = factor(a.k_scale);
     p.fv = factor(a.v_scale);
-    const int32_t width = vec ? 8 : 2;
-    p.q_columns = a.q ? a.n_heads * (a.head_dim / width) : 0;
-    p.k_columns = a.n_kv_heads * (a.head_dim / width);
-    p.v_columns = a.n_kv_heads * (a.head_dim / 4);
+    p.q_columns = plan.q_columns;
+    p.k_columns = plan.k_columns;
+    p.v_columns = plan.v_columns;
+    p.q_parts = plan.q_parts;
+    p.k_parts = plan.k_parts;
+    p.per = plan.per;
+    p.v_per = plan.v_per;
+    const int32_t width = plan.vec ? 8 : 2;
     p.inv_qk = (float)width / a.head_dim;
     p.inv_value = 4.0f / a.head_dim;
     p.inv_half = p.half ? 1.0f / p.half : 0.0f;
-    const bool step = a.max_new == 1;
-    // (the first may begin anywhere in 16 slots; a launch of fewer goes through them in turns)
-    const int64_t groups = step ? 1 : std::min<int64_t>(((int64_t)a.max_new + 30) / 16, kMostGrid);
-    // Columns of a workgroup: in a step one a thread; else as many as leave 4096 workgroups, since each of them computes
-    // its tokens' angles (4 x 4096 tokens of 32 heads of 128 that 4 share: 99.5 us from fp32 and 54 from int8; with 1024
-    // 105.8 and 52, with 16384 98 and 73; ragged prompts, which have fewer in all, 17.7 to 17.8).
-    const auto even = [](int32_t columns, int32_t most) {  // in equal parts of at most so many
-        const int32_t parts = std::max((columns + most - 1) / most, 1);
-        return std::max((columns + parts - 1) / parts, 1);
-    };
-    const double tokens = std::min((double)groups * a.n_seq, (double)a.m_tokens / 16 + a.n_seq);
-    int32_t most = 256;
-    if (!step)
-        while (most > 64 && tokens * (p.q_columns + p.k_columns + p.v_columns) / most < 4096) most /= 2;
-    p.per = even(std::max(p.q_columns, p.k_columns), most);
-    p.v_per = even(p.v_columns, most);
-    p.q_parts = (p.q_columns + p.per - 1) / p.per;
-    p.k_parts = (p.k_columns + p.per - 1) / p.per;
-    const int32_t parts = p.q_parts + p.k_parts + (p.v_columns + p.v_per - 1) / p.v_per;
-    if ((double)groups * a.n_seq * parts > 0x7fffffff / 256) {
-        set_error("too many work items for one launch");
-        return SL_ERR_UNSUPPORTED;
-    }
     const hipStream_t s = static_cast<hipStream_t>(stream);
     for (int64_t s0 = 0; s0 < a.n_seq; s0 += kMostGrid) {
         p.seq0 = (int32_t)s0;
-        const dim3 grid((uint32_t)parts, (uint32_t)groups, (uint32_t)std::min(a.n_seq - p.seq0, kMostGrid));
+        const dim3 grid((uint32_t)plan.parts, (uint32_t)plan.groups, (uint32_t)std::min(a.n_seq - p.seq0, kMostGrid));
         const auto run = [&](auto types, auto widths) {
             constexpr bool F = decltype(types)::value, V = decltype(widths)::value;
-            if (step)
+            if (plan.step)
                 hipLaunchKernelGGL((cache_append_step_kernel<F, V>), grid, dim3(256), 0, s, p);
             else
                 hipLaunchKernelGGL((cache_append_kernel<F, V>), grid, dim3(256), 0, s, p);
         };
-        if (f32 && vec)
+        if (f32 && plan.vec)
             run(std::true_type{}, std::true_type{});
         else if (f32)
             run(std::true_type{}, std::false_type{});
-        else if (vec)
+        else if (plan.vec)
             run(std::false_type{}, std::true_type{});
         else
             run(std::false_type{}, std::false_type{});

@@ -21,6 +21,25 @@ int main()
     }
 }
 """
+APPEND = r"""
+#include <stdio.h>
+#include "cache_plan.h"
+using namespace sl;
+int main()
+{
+    static int8_t some;
+    int queries;
+    sl_cache_append_args a{};
+    while (scanf("%ld %d %d %d %d %d %d %d %d", &a.m_tokens, &a.n_seq, &a.max_new, &a.n_heads, &a.n_kv_heads, &a.head_dim,
+                 &a.rope_kind, &a.rope_dim, &queries) == 9) {
+        a.q = queries ? &some : nullptr;
+        const AppendPlan p = plan_of(a);
+        printf("%d %d %d %d %d %d %d %d %d %d %d %d\n", p.fits, p.step, p.vec, p.groups, p.q_columns, p.k_columns, p.v_columns,
+               p.q_parts, p.k_parts, p.parts, p.per, p.v_per);
+    }
+}
+"""
+Append = namedtuple("Append", "fits step vec groups q_columns k_columns v_columns q_parts k_parts parts per v_per")
 Attention = namedtuple("Attention", "prompt by_length fits tile_rows splits split_keys tiles")
 
 
@@ -34,7 +53,14 @@ def _program(text):
     return exe
 
 
+def _run(program, given):
+    return map(int, subprocess.run([_program(program)], input=" ".join(map(str, given)), check=True, stdout=subprocess.PIPE,
+                                   text=True).stdout.split())
+
+
 def attention(m_tokens, n_seq, max_new, max_len, n_heads, n_kv_heads, head_dim, causal=True):
-    given = (m_tokens, n_seq, max_new, max_len, n_heads, n_kv_heads, head_dim, int(causal))
-    out = subprocess.run([_program(PROGRAM)], input=" ".join(map(str, given)), check=True, stdout=subprocess.PIPE, text=True)
-    return Attention(*map(int, out.stdout.split()))
+    return Attention(*_run(PROGRAM, (m_tokens, n_seq, max_new, max_len, n_heads, n_kv_heads, head_dim, int(causal))))
+
+
+def append(m_tokens, n_seq, max_new, n_heads, n_kv_heads, head_dim, rope_kind=0, rope_dim=0, queries=True):
+    return Append(*_run(APPEND, (m_tokens, n_seq, max_new, n_heads, n_kv_heads, head_dim, rope_kind, rope_dim, int(queries))))

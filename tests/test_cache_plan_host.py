@@ -18,6 +18,31 @@ def test_one_prompt_beside_steps(n_seq, prompt, nh, nkv, hd):
         assert p.tiles * p.tile_rows <= prompt * (nh // nkv) + p.tile_rows - 1
 
 
+@pytest.mark.parametrize("n_seq,prompt,nh,nkv,hd", [
+    (256, 131072, 32, 8, 128), (2049, 32768, 32, 8, 128), (2, 2 ** 30, 32, 8, 128), (65536, 65536, 12, 12, 64),
+    (1, 2 ** 31 - 256, 16, 4, 64), (4096, 8192, 64, 1, 64)])
+@pytest.mark.parametrize("kind,rot,queries", [(0, 0, True), (1, 64, True), (2, 18, True), (0, 0, False)])
+def test_one_prompt_beside_steps_is_appended(n_seq, prompt, nh, nkv, hd, kind, rot, queries):
+    p = plan.append(n_seq - 1 + prompt, n_seq, prompt, nh, nkv, hd, kind, rot, queries)
+    assert p.fits and not p.step and p.vec == (rot != 18) and 0 < p.groups <= min(GRID, (prompt + 30) // 16)
+    assert n_seq * p.parts * p.groups <= ITEMS
+    v_parts = -(-p.v_columns // p.v_per)
+    assert p.parts == p.q_parts + p.k_parts + v_parts and max(p.per, p.v_per) <= 256
+    for columns, parts, per in ((p.q_columns, p.q_parts, p.per), (p.k_columns, p.k_parts, p.per), (p.v_columns, v_parts, p.v_per)):
+        assert (parts - 1) * per < columns <= parts * per
+
+
+def test_a_launch_of_fewer_groups_than_a_sequence_has():
+    n, _, prompt, nh, nkv, hd = MIXED[0]
+    p = plan.append(n - 1 + prompt, n, prompt, nh, nkv, hd, 1, hd)
+    assert p.fits and 1 < p.groups < prompt // 16
+
+
+def test_more_sequences_than_a_launch_takes():
+    assert plan.append(2 ** 22, 2 ** 22, 1, 1, 1, 16).fits == 0  # 3 workgroups each
+    assert plan.append(2 ** 21, 2 ** 21, 1, 1, 1, 16).fits == 1
+
+
 @pytest.mark.parametrize("n,at,prompt,nh,nkv,hd", MIXED)
 def test_mixed_batches_have_more_tiles_than_workgroups(n, at, prompt, nh, nkv, hd):
     p = plan.attention(n - 1 + prompt, n, prompt, prompt, nh, nkv, hd)

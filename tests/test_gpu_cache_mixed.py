@@ -1,8 +1,9 @@
 """One prompt beside many steps in a call of a decoder's cache: so many sequences that there is no workgroup for each of
-the prompt's tiles times the sequences, against the definition in 64 bits. The bar is test_gpu_cache.py's."""
+the prompt's tiles (or groups of 16 slots) times the sequences, against the definitions in 64 bits. The bars are
+test_gpu_cache.py's."""
 import pytest
 
-from test_gpu_cache import FILL, TOL
+from test_gpu_cache import DELTA, FILL, TOL
 
 pytestmark = pytest.mark.gpu
 
@@ -79,3 +80,48 @@ def test_attention(hip, n, at, prompt, nh, nkv, hd, causal):
                 z.masked_fill_(later, -torch.inf)
             worst = max(worst, float((y[b.rows, head] - torch.softmax(z, 1) @ v * f(vs)).abs().max()))
     assert worst <= TOL * vs, worst
+
+
+@pytest.mark.parametrize("x_type", ["i8", "f32"])
+def test_append(hip, x_type):
+    import numpy as np
+    import torch
+    n, at, prompt, nh, nkv, hd = MIXED[0]
+    b = Mixed(hip, n, at, prompt, nkv, hd)
+    b.len[at] = prompt - 5  # (its first five tokens have no slot)
+    f = lambda v: float(np.float32(v))  # noqa: E731
+    xs, qs, ks, vs = 0.031, 0.037, 0.041, 0.031
+    x = b.codes(b.m, (nh + 2 * nkv) * hd)
+    value = (x.double() * f(xs)).reshape(b.m, nh + 2 * nkv, hd)
+    if x_type == "f32":
+        x = value.reshape(b.m, -1).float()
+        value = x.double().reshape(value.shape)
+    freq = torch.tensor(10000.0 ** (-np.arange(hd // 2) * 2 / hd), dtype=torch.float32, device="cuda")
+    before = b.cache.clone()
+    print(f"append of a prompt beside steps: {n} sequences, {prompt} tokens, {x_type}", flush=True)
+    q = hip.cache_append(x, *b.call(), nh, x_scale=xs if x_type == "i8" else 1.0, q_scale=qs, k_scale=ks, v_scale=vs,
+                         rope=hip.ROPE_HALF, inv_freq=freq)
+    torch.cuda.synchronize()
+    # every token's sequence, slot and page
+    seq = torch.repeat_interleave(torch.arange(n, device="cuda"), torch.where(b.steps, 1, prompt))
+    start, lens = b.start.long(), b.len.long()
+    slot = lens[seq] - (start[seq + 1] - start[seq]) + torch.arange(b.m, device="cuda") - start[seq]
+    w = slot.double()[:, None] * freq.double()
+    c, s, (u, v) = w.cos()[:, None], w.sin()[:, None], value[:, :nh + nkv].chunk(2, 2)
+    turned = torch.cat([u * c - v * s, v * c + u * s], 2)
+
+    def near(codes, want, scale):
+        want = (want / f(scale)).clamp(-127, 127)
+        assert float((codes.double() - want).abs().max()) <= 0.5 + DELTA
+
+    near(q.reshape(b.m, nh, hd), turned[:, :nh], qs)
+    put = slot >= 0
+    page, place = b.table[seq[put], slot[put] // PS].long(), slot[put] % PS
+    assert int((~put).sum()) >= 5 and int(page.min()) >= 0
+    near(b.cache[page, 0, :, place], turned[put, nh:], ks)
+    got, was = (t[:, 1].reshape(-1, nkv, hd, PS) for t in (b.cache, before))
+    near(got[page, :, :, place], value[put, nh + nkv:], vs)
+    # what no token of the call is in stays as it was
+    before[page, 0, :, place] = b.cache[page, 0, :, place]
+    was[page, :, :, place] = got[page, :, :, place]
+    assert torch.equal(b.cache[:, 0], before[:, 0]) and torch.equal(got, was)
