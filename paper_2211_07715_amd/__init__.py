@@ -214,6 +214,19 @@ def _stream_ptr(stream) -> int:
     return _raw_stream()
 
 
+def _empty(shape, dtype, device, stream):
+    """Memory of a result that `stream` (None: the current one) writes. For another stream than the current one it is of
+    that stream's, where no earlier work of the current one is on it, and is not handed on before the current one's later
+    work on it."""
+    if stream is None or stream.cuda_stream == _raw_stream():
+        return _torch.empty(shape, dtype=dtype, device=device)
+    current = _torch.cuda.current_stream(device)
+    with _torch.cuda.stream(stream):
+        out = _torch.empty(shape, dtype=dtype, device=device)
+    out.record_stream(current)
+    return out
+
+
 class PackedWeight:
     """An immutable packed 4x1 block-sparse int8 weight (one C handle)."""
 
@@ -635,7 +648,7 @@ def cache_append(x, cache, page_table, seq_start, kv_len, max_new: int, n_heads:
     if q_scale is not None:
         shape = t16x32_shape(m_tokens, n_heads * head_dim) if q_layout == LAYOUT_T16X32 else (m_tokens, n_heads * head_dim)
         if out is None:
-            q = torch.empty(shape, dtype=torch.int8, device=x.device)
+            q = _empty(shape, torch.int8, x.device, stream)
         else:
             q = out
             if q.dtype is not torch.int8 or q.shape != shape or not q.is_contiguous() or q.device != x.device:
@@ -693,7 +706,8 @@ def cache_attention(q, cache, page_table, seq_start, kv_len, max_new: int, max_l
     dt = _KIND_DTYPE.get(kind)
     shape = t16x32_shape(m_tokens, cols) if y_layout == LAYOUT_T16X32 else (m_tokens, cols)
     if out is None:  # (empty_like: 0.6 us less a call)
-        out = torch.empty_like(q) if dt is torch.int8 and have == shape else torch.empty(shape, dtype=dt, device=q.device)
+        out = torch.empty_like(q) if dt is torch.int8 and have == shape and stream is None else \
+            _empty(shape, dt, q.device, stream)
     elif out.dtype is not dt or out.shape != shape or not out.is_contiguous() or out.device != q.device:
         raise ValueError("out has the wrong dtype/shape/device or is not contiguous")
     if softmax_scale is None:
