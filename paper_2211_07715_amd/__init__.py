@@ -34,6 +34,10 @@ cached tokens with the call's own; page_table: the numbers of its pages):
                         k_scale=s_k, v_scale=s_v, rope=sl.ROPE_HALF, inv_freq=inv_freq)
     a = sl.cache_attention(q, cache, page_table, seq_start, kv_len, max_new, max_len, n_heads, q_scale=s_q,
                            k_scale=s_k, v_scale=s_v, out_scale=s_a)      # causal=False: over an encoder's states
+
+Calls run on the current stream, or on `stream`: the caller then orders it behind
+what makes the inputs and before what reads the results. Memory that a call
+allocates for results is that stream's.
 """
 from __future__ import annotations
 
@@ -326,7 +330,7 @@ class PackedWeight:
         dt = _KIND_DTYPE[kind]
         shape = t16x32_shape(m, self.n_out) if y_layout == LAYOUT_T16X32 else (m, self.n_out)
         if out is None:
-            out = torch.empty(shape, dtype=dt, device=x.device)
+            out = _empty(shape, dt, x.device, stream)
         elif out.dtype != dt or tuple(out.shape) != tuple(shape) or not out.is_contiguous():
             raise ValueError("out has the wrong dtype/shape or is not contiguous")
         lib = load()
@@ -365,7 +369,7 @@ def quantize_act(x, scale: float, out=None, stream=None, layout: int = LAYOUT_RO
         raise ValueError("x must be a contiguous CUDA float32 tensor")
     if layout == LAYOUT_ROWS:
         if out is None:
-            out = torch.empty(x.shape, dtype=torch.int8, device=x.device)
+            out = _empty(x.shape, torch.int8, x.device, stream)
         elif out.dtype != torch.int8 or out.numel() != x.numel() or not out.is_contiguous():
             raise ValueError("out must be a contiguous int8 tensor with x's size")
         _check(load().quantize_act(x.data_ptr(), x.numel(), float(scale), out.data_ptr(), _stream_ptr(stream)),
@@ -376,7 +380,7 @@ def quantize_act(x, scale: float, out=None, stream=None, layout: int = LAYOUT_RO
     rows, cols = x.shape
     shape = t16x32_shape(rows, cols)
     if out is None:
-        out = torch.empty(shape, dtype=torch.int8, device=x.device)
+        out = _empty(shape, torch.int8, x.device, stream)
     elif out.dtype != torch.int8 or tuple(out.shape) != shape or not out.is_contiguous():
         raise ValueError(f"out must be a contiguous int8 tensor of shape {shape}")
     _check(load().quantize_act_layout(x.data_ptr(), rows, cols, float(scale), out.data_ptr(), int(layout),
@@ -452,13 +456,13 @@ def residual_norm(y, gamma=None, beta=None, *, norm: int = NORM_LAYER, eps: floa
     channels = (cols,)
     h = u = q = None
     if keep_sum is not False and keep_sum is not None:
-        h = torch.empty(shape, dtype=torch.float32, device=y.device) if keep_sum is True else keep_sum
+        h = _empty(shape, torch.float32, y.device, stream) if keep_sum is True else keep_sum
     if keep_norm is not False and keep_norm is not None:
-        u = torch.empty(shape, dtype=torch.float32, device=y.device) if keep_norm is True else keep_norm
+        u = _empty(shape, torch.float32, y.device, stream) if keep_norm is True else keep_norm
     if out_scale is not None:
         q_shape = t16x32_shape(rows, cols) if q_layout == LAYOUT_T16X32 else shape
         if q_out is None:
-            q = torch.empty(q_shape, dtype=torch.int8, device=y.device)
+            q = _empty(q_shape, torch.int8, y.device, stream)
         else:
             q = q_out
             if q.dtype is not torch.int8 or q.shape != q_shape or not q.is_contiguous() or not q.is_cuda:
@@ -526,7 +530,7 @@ def attention(qkv, x_scale: float, seq_start, max_len: int, n_heads: int, head_d
     dt = _KIND_DTYPE.get(kind)
     shape = t16x32_shape(m, cols) if y_layout == LAYOUT_T16X32 else (m, cols)
     if out is None:
-        out = torch.empty(shape, dtype=dt, device=qkv.device)
+        out = _empty(shape, dt, qkv.device, stream)
     elif out.dtype != dt or tuple(out.shape) != shape or not out.is_contiguous() or not out.is_cuda:
         raise ValueError("out has the wrong dtype/shape or is not contiguous")
     lists, top_k = 0, 0
@@ -561,7 +565,7 @@ def select_blocks(qkv, seq_start, max_len: int, n_heads: int, head_dim: int, top
         raise ValueError("query_block and top_k must be >= 1, n_heads and max_len >= 0")
     shape = (n_seq, n_heads, -(-max_len // query_block), top_k)
     if out is None:
-        out = torch.empty(shape, dtype=torch.int32, device=qkv.device)
+        out = _empty(shape, torch.int32, qkv.device, stream)
     elif out.dtype != torch.int32 or tuple(out.shape) != shape or not out.is_contiguous() or not out.is_cuda:
         raise ValueError(f"out must be a contiguous CUDA int32 tensor of shape {shape}")
     if m == 0:  # (the call writes nothing)

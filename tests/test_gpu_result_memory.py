@@ -30,7 +30,43 @@ def attend(kind, y_layout=0):
     return make
 
 
-CALLS = {"cache_append": append, "cache_attention, codes": attend(3), "cache_attention, blocks": attend(3, 1),
+def linear(kind, y_layout=0):
+    def make(hip, rng):
+        w = rng.integers(-8, 9, (64, 64)).astype(np.int8)
+        packed = hip.PackedWeight.pack(w, np.full(64, 0.01, np.float32))
+        x = cuda(codes(rng, M, 64))
+        return lambda s: (packed.run(x, 0.05, kind, out_scale=0.05, y_layout=y_layout, stream=s),)
+    return make
+
+
+def quantize(layout):
+    def make(hip, rng):
+        x = cuda(rng.standard_normal((M, 64)).astype(np.float32))
+        return lambda s: (hip.quantize_act(x, 0.03, layout=layout, stream=s),)
+    return make
+
+
+def norm(hip, rng):
+    y, r = (cuda(rng.standard_normal((M, 64)).astype(np.float32)) for _ in range(2))
+    gamma, beta = (cuda(rng.standard_normal(64).astype(np.float32)) for _ in range(2))
+    return lambda s: hip.residual_norm(y, gamma, beta, residual=r, keep_sum=True, keep_norm=True, out_scale=0.03, stream=s)
+
+
+def encoder(kind):
+    def make(hip, rng):
+        x, start = cuda(codes(rng, M, 3 * 128)), cuda(np.arange(0, M + 1, 50, dtype=np.int32))
+        return lambda s: (hip.attention(x, 0.03, start, 50, 2, 64, kind=kind, out_scale=0.03, stream=s),)
+    return make
+
+
+def select(hip, rng):
+    x, start = cuda(codes(rng, M, 3 * 128)), cuda(np.arange(0, M + 1, 400, dtype=np.int32))
+    return lambda s: (hip.select_blocks(x, start, 400, 2, 64, 200, query_block=16, stream=s),)
+
+
+CALLS = {"run, fp32": linear(1), "run, codes": linear(3), "run, blocks": linear(3, 1), "quantize_act": quantize(0),
+         "quantize_act, blocks": quantize(1), "residual_norm": norm, "attention, fp32": encoder(1),
+         "attention, codes": encoder(3), "select_blocks": select, "cache_append": append, "cache_attention, codes": attend(3), "cache_attention, blocks": attend(3, 1),
          "cache_attention, fp32": attend(1)}
 
 
@@ -75,9 +111,9 @@ def test_results_on_the_current_stream_by_name(hip, name):
     s.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(s):
         got = call(s)
-        at = [t.data_ptr() for t in got]
+        at = {t.data_ptr() for t in got}
         kept = [t.clone() for t in got]
         del got
-        assert [t.data_ptr() for t in call(s)] == at
+        assert {t.data_ptr() for t in call(s)} == at
     torch.cuda.synchronize()
     assert all(torch.equal(g, w) for g, w in zip(kept, want))
