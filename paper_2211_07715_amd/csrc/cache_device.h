@@ -32,7 +32,7 @@ struct CacheArgs {
     int32_t n_seq, tiles, splits, split_keys;
     int32_t n_heads, n_kv, group, hd, q_cols, q_cb, y_cb, shift, max_pages, n_pages, causal, y_f32, tile_rows, join_group, seq0, group_shift;
     int32_t by_length;  // tiles in order of the keys that they see
-    float c2, k2, vs, inv_so, inv_group;
+    float c2, k2, vs, unit, inv_group;
 };
 
 // cache_attention for many queries a sequence (kernels_cache_prompt.hip): tile_rows, 64 or 128, (query, head) pairs a

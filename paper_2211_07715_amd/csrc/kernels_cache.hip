@@ -38,6 +38,7 @@
 // up to 4096 of 8 heads of 128 55 (4.6), 32 x 384 tokens of 12 heads of 64 8.4, 128
 // tokens 4.7. Vector instructions are active 30 % of the time
 // in the first, matrix ones 7 %.
+#include <float.h>
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -457,13 +458,13 @@ constexpr int32_t kNone = -(1 << 30);  // m without a key
 // One output row's share: query row, 4 features from c on
 __device__ __forceinline__ void store_row(const CacheArgs &a, int64_t tok, int32_t head, int32_t c, f32x4 v, float l)
 {
-    const float g = l > 0.0f ? a.vs / l : 0.0f;
+    const float g = l > 0.0f ? a.vs / l : 0.0f;  // (under 4, as unit times it is finite)
     const int32_t cols = a.n_heads * a.hd;
     if (a.y_f32)
-        *reinterpret_cast<f32x4 *>(static_cast<float *>(a.y) + tok * cols + head * a.hd + c) = v * g;
+        *reinterpret_cast<f32x4 *>(static_cast<float *>(a.y) + tok * cols + head * a.hd + c) = v * g * a.unit;
     else
         *reinterpret_cast<uint32_t *>(static_cast<int8_t *>(a.y) + at(tok, head * a.hd + c, cols, a.y_cb)) =
-            codes_of(v, g * a.inv_so);
+            codes_of(v, g * a.unit);
 }
 
 // SORTED: where sequences turn out to differ in length, those that see the most keys come first.
@@ -847,7 +848,10 @@ sl_status launch_cache_append(const sl_cache_append_args &a, void *stream)
     p.half = a.rope_kind != SL_ROPE_NONE ? a.rope_dim / 2 : 0;
     p.split = a.rope_kind == SL_ROPE_HALF;
     p.rope_factor = a.rope_factor;
-    const auto factor = [&](float scale) { return f32 ? 1.0f / scale : (float)((double)a.x_scale / scale); };
+    // (finite, so that 0 stays 0; what it cuts is a code of 127 all the same)
+    const auto factor = [&](float scale) {
+        return std::min(f32 ? 1.0f / scale : (float)std::min((double)a.x_scale / scale, (double)FLT_MAX), FLT_MAX);
+    };
     p.fq = factor(a.q_scale);
     p.fk = factor(a.k_scale);
     p.fv = factor(a.v_scale);
@@ -919,8 +923,12 @@ sl_status launch_cache_attention(const sl_cache_attention_args &args, void *stre
     a.causal = args.causal;
     a.y_f32 = args.kind == SL_EPI_F32;
     a.c2 = (float)((double)args.q_scale * args.k_scale * args.softmax_scale * 1.4426950408889634);
-    a.vs = args.v_scale;
-    a.inv_so = a.y_f32 ? 1.0f : 1.0f / args.out_scale;
+    // A result is a mean of codes (vs / l times their sum) times `unit`, where vs is v_scale's mantissa, 1 .. 2, and unit has
+    // its exponent: v_scale / l may be less than a float holds in full, and v_scale / out_scale more than one.
+    int ev = 0, eo = 0;
+    a.vs = 2.0f * frexpf(args.v_scale, &ev);
+    const float mo = a.y_f32 ? 1.0f : 2.0f * frexpf(args.out_scale, &eo);
+    a.unit = (float)std::min(ldexp((double)(1.0f / mo), a.y_f32 ? ev - 1 : ev - eo), a.y_f32 ? (double)FLT_MAX : (double)FLT_MAX / 4);
     a.inv_group = 1.0f / a.group;
     a.group_shift = (a.group & (a.group - 1)) ? -1 : __builtin_ctz(a.group);
     a.tile_rows = p.tile_rows;

@@ -437,7 +437,7 @@ void cache_prompt_kernel(const CacheArgs a)
             }
             continue;
         }
-        const float f = sum > 0.0f ? a.vs / sum * a.inv_so : 0.0f;
+        const float mean = sum > 0.0f ? a.vs / sum : 0.0f, f = mean * a.unit;
         const int32_t cols = a.n_heads * a.hd;
         if (i < 0) continue;
         const int64_t tok = (int64_t)tk.first + i;
@@ -449,7 +449,7 @@ void cache_prompt_kernel(const CacheArgs a)
                 float *y = static_cast<float *>(a.y) + tok * cols + q_head * a.hd + f0;
 #pragma unroll
                 for (int e = 0; e < 16; e += 4)
-                    *reinterpret_cast<f32x4 *>(y + e) = f32x4{o[d][e], o[d][e + 1], o[d][e + 2], o[d][e + 3]} * f;
+                    *reinterpret_cast<f32x4 *>(y + e) = f32x4{o[d][e], o[d][e + 1], o[d][e + 2], o[d][e + 3]} * mean * a.unit;
             } else {
                 i32x4 w;
 #pragma unroll
