@@ -4,6 +4,7 @@ import pytest
 
 import cache_plan as plan
 from test_gpu_cache_mixed import MIXED
+from test_gpu_cache_order import PROMPTS, STEPS, said
 
 ITEMS, GRID = 2 ** 23 - 1, 65535
 
@@ -58,3 +59,23 @@ def test_what_fits_has_a_workgroup_for_every_tile():
 def test_one_tile_a_sequence_does_not_fit():
     assert plan.attention(2 ** 20, 2 ** 20, 1, 64, 8, 8, 64).fits == 0  # 2^23 tiles
     assert plan.attention(2 ** 20, 2 ** 20 - 1, 1, 64, 8, 8, 64).fits == 1
+
+
+@pytest.mark.parametrize("name", [*PROMPTS, *STEPS])
+@pytest.mark.parametrize("causal", [True, False])
+def test_what_is_to_be_in_order_is(name, causal):
+    case = {**PROMPTS, **STEPS}[name]
+    p = plan.attention(*said(case), causal)
+    assert p.fits and p.by_length and p.prompt == (name in PROMPTS)
+    assert (p.splits > 1) == ("parts" in name or name in STEPS)
+    if name in STEPS:
+        assert p.tiles == int(name[name.index("of") + 3])
+    (news, _), nh, nkv, *_ = case
+    assert ("more tokens" in name) == (max(news) * (nh // nkv) > p.tiles * p.tile_rows)
+
+
+def test_the_paths_of_the_order_tests_cover_both_tables_of_lengths():
+    n = [len(case[0][0]) for case in PROMPTS.values()], [len(case[0][0]) for case in STEPS.values()]
+    assert all(min(c) <= 64 < max(c) <= 256 for c in n) and max(n[0]) == 256
+    rows = {plan.attention(*said(case)).tile_rows for case in PROMPTS.values()}
+    assert rows == {64, 128}
