@@ -79,3 +79,10 @@ def test_the_paths_of_the_order_tests_cover_both_tables_of_lengths():
     assert all(min(c) <= 64 < max(c) <= 256 for c in n) and max(n[0]) == 256
     rows = {plan.attention(*said(case)).tile_rows for case in PROMPTS.values()}
     assert rows == {64, 128}
+
+
+def test_forms_of_the_bar_tests():
+    p = plan.attention(9, 4, 5, 256, 8, 2, 64)
+    assert not p.prompt and p.splits == 1
+    for hd in range(16, 129, 16):
+        assert plan.attention(238 * 6, 30, 130, 200, 12, 6, hd).prompt
