@@ -394,8 +394,9 @@ typedef enum {
  *   q           [m_tokens x n_heads * head_dim] int8 in q_layout, 16-byte aligned,
  *               or NULL: not written. Padding and tokens of no sequence are left
  *               as they are.
- *   max_new     largest n_s: what the launch is sized by (longer sequences are
- *               still done whole; 0: no-op)
+ *   max_new     largest n_s: what the launch is sized by, n_seq * max_new tokens (a
+ *               long prompt and many steps are faster in a call each; longer
+ *               sequences are still done whole; 0: no-op)
  *   max_pages   entries of page_table a sequence, max_pages * page_size at most
  *               2^31 - 65536
  *   page_size   16, 32, 64, 128 or 256
@@ -453,7 +454,8 @@ sl_status cache_append(const sl_cache_append_args *args, void *hip_stream);
  *   q_cols      >= n_heads * head_dim, row-major a multiple of 16, at most 2^24
  *   max_new     largest n_s, as in cache_append
  *   max_len     largest kv_len: with max_new what the launch is sized by (longer
- *               ones are still computed whole)
+ *               ones are still computed whole). It also fixes how keys are cut into
+ *               parts: a bound far over the lengths gives the same results slower
  *   causal      0 or 1
  *   kind        SL_EPI_F32 (y fp32, row-major) or SL_EPI_I8 (codes of out_scale in
  *               y_layout)

@@ -686,8 +686,8 @@ def cache_attention(q, cache, page_table, seq_start, kv_len, max_new: int, max_l
     """Attention of a call's tokens (query codes [M, n_heads * head_dim] of q_scale, or wider rows that begin with them:
     q_cols, in the block layout) over what their sequences have in the cache: one token a sequence, some, or prompts.
 
-    Sequences as in cache_append; max_new and max_len, the largest of their tokens and of kv_len, size the launch. With
-    causal a token sees the slots up to its own, else all kv_len[s] (an encoder's states). softmax_scale: default
+    Sequences as in cache_append; max_new and max_len, the largest of their tokens and of kv_len, size the launch (what is
+    longer is still done whole; a bound far over the lengths, or a long prompt among many steps, takes longer). With causal a token sees the slots up to its own, else all kv_len[s] (an encoder's states). softmax_scale: default
     1 / sqrt(head_dim). Returns [M, n_heads * head_dim]: int8 codes of out_scale (EPI_I8, y_layout) or fp32 (EPI_F32); 0
     where nothing is seen. Tokens of no sequence are left as they are."""
     torch = _torch or _torch_once()
