@@ -117,3 +117,31 @@ def test_results_on_the_current_stream_by_name(hip, name):
         assert {t.data_ptr() for t in call(s)} == at
     torch.cuda.synchronize()
     assert all(torch.equal(g, w) for g, w in zip(kept, want))
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_results_on_another_stream_of_a_captured_graph(hip, name):
+    """A call on a stream that a capture forks to, its results used where the streams meet; replayed several times, with
+    eager work between."""
+    import torch
+    call = CALLS[name](hip, np.random.default_rng(3))
+    want = [t.clone() for t in call(None)]
+    torch.cuda.synchronize()
+    main, side = torch.cuda.Stream(), torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=main):
+        side.wait_stream(main)
+        first = call(side)
+        main.wait_stream(side)
+        kept = [t.clone() for t in first]
+        del first
+        side.wait_stream(main)
+        second = call(side)
+        main.wait_stream(side)
+    for _ in range(4):
+        for t in (*kept, *second):
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(k, w) and torch.equal(s, w) for k, s, w in zip(kept, second, want))
+        assert all(torch.equal(t, w) for t, w in zip(call(None), want))
